@@ -275,6 +275,106 @@ kvc_status kvc_compress(const kvc_params* params, const kvc_inputs* in,
                         const kvc_outputs* out, void* workspace,
                         size_t workspace_bytes, void* stream);
 
+/* ---- the 8-bit block cache: what the pass keeps, while an answer is decoded ----
+ *
+ * A pool of blocks of KVC_BLOCK_TOKENS tokens, each of Hb heads:
+ *   k        device, uint8 [blocks, Hb, 64, d]   codes of K, token by token
+ *   v        device, uint8 [blocks, Hb, d, 64]   codes of V, dimension by dimension
+ *   k_scale, v_scale  device, float [blocks, Hb] scale of the codes of a block and head
+ *   weight   device, float [blocks, Hb, 64]      attention weight that a token has gathered; may be
+ *                                                NULL where nothing is evicted
+ *   table    device, int32 [rows, table_width]   blocks of a row in the order of its tokens
+ * A row is a (sequence, layer), b*Lyr + l, and Hb = Hkv; with unstructured = 1 it is a (sequence,
+ * layer, head), (b*Lyr + l)*Hkv + h, and Hb = 1.  lengths is device int32 [rows] everywhere: the
+ * tokens of a row, in the layout that kvc_global_select and kvc_compress write.  Token t of a row
+ * is slot t % 64 of block table[row, t / 64].
+ *
+ * A code stands for code * scale.  Scales are powers of two: the least 2^e, e >= -100, for which the
+ * block's largest magnitude is at most top * 2^e (top = 448 for KVC_E4M3, 127 for KVC_INT8); codes are
+ * value / scale rounded to nearest, halves to even.  Non-finite values are undefined.
+ *
+ * Nothing is read or written outside the pools whatever lengths and table hold: a length is taken
+ * between 0 and table_width*64, and a table entry outside [0, blocks) is not followed (its tokens are
+ * absent: not attended to, not written, weight -infinity when evicting).  Slots behind a row's last
+ * token may hold anything.  Rows may share blocks that are only read; a block that a call writes must
+ * belong to one row, once.  Calls on the same blocks are ordered by their streams.  A captured
+ * call reads lengths and tables when it is replayed.
+ *
+ * Additional limits: d a multiple of 16; k and v of the cache 16-byte aligned; table_width < 2^23.
+ * Used of params: batch, layers, hq, hkv, head_dim, dtype (of rows, queries and outputs), unstructured,
+ * and what each function names. */
+#define KVC_BLOCK_TOKENS 64
+typedef enum {
+  KVC_E4M3 = 0, /* OCP 8-bit floating point: 4 exponent, 3 mantissa bits */
+  KVC_INT8 = 1  /* whole numbers -127 .. 127 */
+} kvc_format;
+
+typedef struct kvc_cache {
+  int32_t format;      /* kvc_format of the codes */
+  int32_t blocks;      /* blocks in the pools */
+  int32_t table_width; /* entries of a row of the table */
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  float* weight;
+  const int32_t* table;
+} kvc_cache;
+
+/* Stage 5 into the cache: rows idx[l,h,0..N_{b,l}) of K and V, in that order or (params->order =
+ * KVC_ORDER_POSITION) in ascending position, become the tokens of their row.  Arguments as those of
+ * kvc_gather, in whose place it stands; idx may be NULL: the first N_{b,l} tokens as they lie.  The
+ * rest of a row's last block is cleared.  Where the cache has weights, a token starts with
+ * scores[l,h,position] (scores: device float [Lyr,Hkv,T], for instance S), or 0 if scores is NULL. */
+kvc_status kvc_cache_fill(const kvc_params* params, const void* const* k, const void* const* v,
+                          const int32_t* idx, const float* scores, const int32_t* lengths,
+                          const int64_t* offsets, const int64_t* cu_seqlens, int64_t total_budget,
+                          const kvc_cache* cache, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/* Appends M = params->window tokens to layer `layer` of every sequence.  k_new, v_new: device
+ * [Bt, Hkv, M, d].  lengths counts the new tokens already (add M before the call): new token m
+ * is token lengths[row] - M + m of its row, those that would lie before token 0 are left out (a padded
+ * sequence has length 0), and a row longer than its table takes none.  A block that already holds
+ * tokens keeps its scale unless a new token needs a larger one; then its codes are rounded again
+ * to the larger scale.  New tokens have weight 0.  A call repeated with the same arguments changes nothing. */
+kvc_status kvc_cache_append(const kvc_params* params, int32_t layer, const void* k_new,
+                            const void* v_new, const int32_t* lengths, const kvc_cache* cache,
+                            void* stream);
+
+/* Attention of M = params->window query tokens of layer `layer` over the cache.  q, out: device
+ * [Bt, Hq, M, d].  Every query sees all tokens of its row or, with causal_tail = 1, query m the
+ * first lengths[row] - M + 1 + m (the queries are the row's last M tokens).  Scale: softmax_scale.
+ *   max_length  host: no row is read beyond so many tokens (sizes the launch and the workspace;
+ *               what exceeds the table counts as the table's capacity)
+ *   lse         device float [Bt, Hq, M] or NULL: logarithm of the sum of exp(logits)
+ *   weight_out  device, laid out as the cache's weight, or NULL: for every token c of the row
+ *               weight_out[c] = weight_in[c] + sum over the M queries and the G heads of its KV
+ *               head of the probability of c.  weight_in NULL counts as 0; both may be the cache's weight.
+ * A query that sees no token gives out = 0 and lse = -infinity.  Products on the bf16 matrix cores
+ * with fp32 accumulation: codes are bf16 numbers exactly, bf16 calls round probabilities to bf16 for
+ * the product with V, fp32 calls split queries and probabilities into three bf16 terms. */
+kvc_status kvc_cache_attend(const kvc_params* params, int32_t layer, const void* q,
+                            const int32_t* lengths, int64_t max_length, const kvc_cache* cache,
+                            void* out, float* lse, const float* weight_in, float* weight_out,
+                            void* workspace, size_t workspace_bytes, void* stream);
+/* Bytes of workspace of such a call; weights: 1 if weight_out is given. */
+kvc_status kvc_cache_attend_workspace(const kvc_params* params, int64_t max_length, int32_t weights,
+                                      size_t* bytes);
+
+/* Cuts all rows (every sequence and layer) back to min(keep[row], max_keep, lengths[row]) tokens; every
+ * head keeps its own.  The first params->keep_first and the last keep_last tokens of a row count
+ * as +infinity, the others by their weight; the largest stay, equal ones in ascending position, and
+ * keep their order and weights.  keep: device int32 [rows].  The kept tokens are written to the blocks
+ * of table_out (device int32 [rows, table_width], same pools), none of which may belong to a row of
+ * the table; the rest of a last block is cleared, lengths_out[row] is set and must not be lengths.
+ * A value keeps its code times scale exactly unless its new block has a larger scale. */
+kvc_status kvc_cache_evict(const kvc_params* params, const int32_t* lengths, const int32_t* keep,
+                           int64_t max_keep, const kvc_cache* cache, const int32_t* table_out,
+                           int32_t* lengths_out, void* workspace, size_t workspace_bytes,
+                           void* stream);
+kvc_status kvc_cache_evict_workspace(const kvc_params* params, int64_t max_keep, size_t* bytes);
+
 /* ---- optional per-kernel timing (measurement aid, not part of the pass) ----
  * While enabled, every kernel the library launches on the calling thread is
  * bracketed by a pair of HIP events recorded on the launch stream.

@@ -15,6 +15,8 @@ from typing import Optional, Sequence
 KVC_F32, KVC_BF16 = 0, 1
 KVC_AGG_MAX, KVC_AGG_MEAN = 0, 1
 KVC_ORDER_RANK, KVC_ORDER_POSITION = 0, 1
+KVC_E4M3, KVC_INT8 = 0, 1
+KVC_BLOCK_TOKENS = 64
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -48,6 +50,16 @@ class KvcParams(C.Structure):
         super().__init__(batch, layers, hq, hkv, head_dim, window, dtype, agg_task, agg_group,
                          agg_head, add_head_mean, softmax_scale, value_norm, order,
                          min_per_layer, unstructured, causal_tail, keep_first, keep_last)
+
+
+class KvcCache(C.Structure):
+    _fields_ = [("format", C.c_int32), ("blocks", C.c_int32), ("table_width", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("weight", C.c_void_p), ("table", C.c_void_p)]
+
+    def __init__(self, format, blocks, table_width, k, v, k_scale, v_scale, weight, table):
+        super().__init__(format, blocks, table_width, *[int(x) if x else None
+                                                        for x in (k, v, k_scale, v_scale, weight, table)])
 
 
 class _Inputs(C.Structure):
@@ -96,7 +108,15 @@ def lib() -> C.CDLL:
         L.kvc_gather.argtypes = [pp, ptab, ptab, vp, vp, vp, i64p, C.c_int64, vp, vp, vp,
                                  C.c_size_t, vp]
         L.kvc_compress.argtypes = [pp, C.POINTER(_Inputs), C.POINTER(_Outputs), vp, C.c_size_t, vp]
-        for name in ("kvc_workspace_size", "kvc_score", "kvc_head_rank", "kvc_composite",
+        pc, i32, i64, size = C.POINTER(KvcCache), C.c_int32, C.c_int64, C.POINTER(C.c_size_t)
+        L.kvc_cache_fill.argtypes = [pp, ptab, ptab, vp, vp, vp, vp, i64p, i64, pc, vp, C.c_size_t, vp]
+        L.kvc_cache_append.argtypes = [pp, i32, vp, vp, vp, pc, vp]
+        L.kvc_cache_attend.argtypes = [pp, i32, vp, vp, i64, pc, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.kvc_cache_attend_workspace.argtypes = [pp, i64, i32, size]
+        L.kvc_cache_evict.argtypes = [pp, vp, vp, i64, pc, vp, vp, vp, C.c_size_t, vp]
+        L.kvc_cache_evict_workspace.argtypes = [pp, i64, size]
+        for name in ("kvc_cache_fill", "kvc_cache_append", "kvc_cache_attend", "kvc_cache_attend_workspace",
+                     "kvc_cache_evict", "kvc_cache_evict_workspace", "kvc_workspace_size", "kvc_score", "kvc_head_rank", "kvc_composite",
                      "kvc_global_select", "kvc_global_select_static", "kvc_gather", "kvc_compress"):
             getattr(L, name).restype = C.c_int
         _LIB = L
@@ -203,6 +223,48 @@ def kvc_compress(params, q, k, v, cu_seqlens, budget, k_out, v_out, lengths, off
                                tau)])
     _check(lib().kvc_compress(C.byref(params), C.byref(inp), C.byref(out), _vp(workspace),
                               workspace_bytes, _vp(stream)), "kvc_compress")
+
+
+def _ref(struct):
+    return C.byref(struct) if struct is not None else None
+
+
+def kvc_cache_fill(params, k, v, idx, lengths, offsets, cu_seqlens, total_budget, cache, stream=0, scores=0,
+                   workspace=0, workspace_bytes=0):
+    _check(lib().kvc_cache_fill(_ref(params), _ptr_table(k), _ptr_table(v), _vp(idx), _vp(scores), _vp(lengths),
+                                _vp(offsets), _i64(cu_seqlens), total_budget, _ref(cache), _vp(workspace),
+                                workspace_bytes, _vp(stream)), "kvc_cache_fill")
+
+
+def kvc_cache_append(params, layer, k_new, v_new, lengths, cache, stream=0):
+    _check(lib().kvc_cache_append(_ref(params), layer, _vp(k_new), _vp(v_new), _vp(lengths), _ref(cache),
+                                  _vp(stream)), "kvc_cache_append")
+
+
+def kvc_cache_attend_workspace(params, max_length, weights=False) -> int:
+    out = C.c_size_t(0)
+    _check(lib().kvc_cache_attend_workspace(_ref(params), max_length, int(weights), C.byref(out)),
+           "kvc_cache_attend_workspace")
+    return out.value
+
+
+def kvc_cache_attend(params, layer, q, lengths, max_length, cache, out, workspace, workspace_bytes, stream=0,
+                     lse=0, weight_in=0, weight_out=0):
+    _check(lib().kvc_cache_attend(_ref(params), layer, _vp(q), _vp(lengths), max_length, _ref(cache), _vp(out),
+                                  _vp(lse), _vp(weight_in), _vp(weight_out), _vp(workspace), workspace_bytes,
+                                  _vp(stream)), "kvc_cache_attend")
+
+
+def kvc_cache_evict_workspace(params, max_keep) -> int:
+    out = C.c_size_t(0)
+    _check(lib().kvc_cache_evict_workspace(_ref(params), max_keep, C.byref(out)), "kvc_cache_evict_workspace")
+    return out.value
+
+
+def kvc_cache_evict(params, lengths, keep, max_keep, cache, table_out, lengths_out, workspace, workspace_bytes,
+                    stream=0):
+    _check(lib().kvc_cache_evict(_ref(params), _vp(lengths), _vp(keep), max_keep, _ref(cache), _vp(table_out),
+                                 _vp(lengths_out), _vp(workspace), workspace_bytes, _vp(stream)), "kvc_cache_evict")
 
 
 class _ProfileEntry(C.Structure):

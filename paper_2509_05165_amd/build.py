@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvc.so")
 SOURCES = ["kvc_api.hip", "kvc_score.hip", "kvc_rank.hip", "kvc_select.hip", "kvc_gather.hip",
-           "kvc_probe.hip"]
+           "kvc_cache_store.hip", "kvc_cache_attend.hip", "kvc_cache_evict.hip", "kvc_probe.hip"]
 
 
 def hipcc() -> str:

@@ -9,6 +9,7 @@
 #include <string>
 #include <vector>
 
+#include "kvc_cache.h"
 #include "kvc_internal.h"
 
 namespace kvc {
@@ -97,6 +98,20 @@ static kvc_status check_params(const kvc_params* p) {
   return KVC_OK;
 }
 
+// What the params say; p has passed check_params.
+static void describe(const kvc_params* p, Problem* pb) {
+  pb->batch = p->batch; pb->layers = p->layers; pb->hq = p->hq; pb->hkv = p->hkv;
+  pb->group = p->hq / p->hkv; pb->d = p->head_dim; pb->window = p->window;
+  pb->dtype = p->dtype; pb->agg_task = p->agg_task; pb->agg_group = p->agg_group;
+  pb->agg_head = p->agg_head; pb->add_head_mean = p->add_head_mean;
+  pb->value_norm = p->value_norm; pb->order = p->order; pb->min_per_layer = p->min_per_layer;
+  pb->unstructured = p->unstructured; pb->causal_tail = p->causal_tail;
+  pb->keep_first = p->keep_first; pb->keep_last = p->keep_last;
+  pb->sel_rows = p->unstructured ? p->layers * p->hkv : p->layers;
+  pb->scale = p->softmax_scale > 0.0f ? p->softmax_scale
+                                      : 1.0f / std::sqrt(float(p->head_dim));
+}
+
 static kvc_status make_problem(const kvc_params* p, const int64_t* cu, Problem* pb) {
   kvc_status st = check_params(p);
   if (st != KVC_OK) return st;
@@ -118,16 +133,7 @@ static kvc_status make_problem(const kvc_params* p, const int64_t* cu, Problem* 
   if (mx >= (int64_t(1) << 29)) {   // 8-byte items of one sequence are addressed with 32-bit byte offsets
     set_error("every sequence must be shorter than 2^29 tokens"); return KVC_ERR_UNSUPPORTED;
   }
-  pb->batch = p->batch; pb->layers = p->layers; pb->hq = p->hq; pb->hkv = p->hkv;
-  pb->group = p->hq / p->hkv; pb->d = p->head_dim; pb->window = p->window;
-  pb->dtype = p->dtype; pb->agg_task = p->agg_task; pb->agg_group = p->agg_group;
-  pb->agg_head = p->agg_head; pb->add_head_mean = p->add_head_mean;
-  pb->value_norm = p->value_norm; pb->order = p->order; pb->min_per_layer = p->min_per_layer;
-  pb->unstructured = p->unstructured; pb->causal_tail = p->causal_tail;
-  pb->keep_first = p->keep_first; pb->keep_last = p->keep_last;
-  pb->sel_rows = p->unstructured ? p->layers * p->hkv : p->layers;
-  pb->scale = p->softmax_scale > 0.0f ? p->softmax_scale
-                                      : 1.0f / std::sqrt(float(p->head_dim));
+  describe(p, pb);
   pb->total = cu[p->batch];
   pb->max_seqlen = mx;
   pb->seq.batch = p->batch;
@@ -171,6 +177,57 @@ static kvc_status check_budget(const Problem& pb, const int64_t* cu, const int64
     sum += budget[b];
   }
   if (total) *total = sum;
+  return KVC_OK;
+}
+
+// A call on the 8-bit block cache: params, cache and (where it works on one) layer.
+static kvc_status make_cache(const kvc_params* p, const kvc_cache* cache, CacheView* c) {
+  if (p->head_dim % 16 != 0) {
+    set_error("head_dim %d unsupported by the block cache (a multiple of 16 is needed)", p->head_dim);
+    return KVC_ERR_UNSUPPORTED;
+  }
+  if (!cache) { set_error("cache is NULL"); return KVC_ERR_INVALID_ARG; }
+  if (cache->format != KVC_E4M3 && cache->format != KVC_INT8) {
+    set_error("unknown cache format %d", cache->format); return KVC_ERR_INVALID_ARG;
+  }
+  if (cache->blocks < 1 || cache->table_width < 1) {
+    set_error("cache blocks and table_width must be positive"); return KVC_ERR_INVALID_ARG;
+  }
+  if (!cache->k || !cache->v || !cache->k_scale || !cache->v_scale || !cache->table) {
+    set_error("k, v, k_scale, v_scale or table of the cache is NULL"); return KVC_ERR_INVALID_ARG;
+  }
+  if ((reinterpret_cast<uintptr_t>(cache->k) | reinterpret_cast<uintptr_t>(cache->v)) % 16 != 0) {
+    set_error("k and v of the cache must be 16-byte aligned"); return KVC_ERR_INVALID_ARG;
+  }
+  if (cache->table_width >= (1 << 23)) {
+    set_error("a table of 2^23 blocks or more per row is unsupported"); return KVC_ERR_UNSUPPORTED;
+  }
+  c->k = static_cast<uint8_t*>(cache->k); c->v = static_cast<uint8_t*>(cache->v);
+  c->k_scale = cache->k_scale; c->v_scale = cache->v_scale; c->weight = cache->weight;
+  c->table = cache->table; c->blocks = cache->blocks; c->width = cache->table_width;
+  c->hkv = p->hkv; c->hb = p->unstructured ? 1 : p->hkv; c->d = p->head_dim; c->layers = p->layers;
+  return KVC_OK;
+}
+
+static kvc_status make_cache_problem(const kvc_params* p, const kvc_cache* cache, Problem* pb, CacheView* c) {
+  kvc_status st = check_params(p);
+  if (st != KVC_OK) return st;
+  describe(p, pb);
+  return make_cache(p, cache, c);
+}
+
+static kvc_status check_layer(const Problem& pb, int32_t layer) {
+  if (layer < 0 || layer >= pb.layers) {
+    set_error("layer %d outside [0, %d)", layer, pb.layers); return KVC_ERR_INVALID_ARG;
+  }
+  return KVC_OK;
+}
+
+// A token count that a row of the table is to hold.
+static kvc_status check_tokens(const char* name, int64_t n, int32_t table_width) {
+  if (n < 0 || n > int64_t(table_width) * KVC_BLOCK_TOKENS) {
+    set_error("%s=%lld outside [0, table_width*64]", name, (long long)n); return KVC_ERR_INVALID_ARG;
+  }
   return KVC_OK;
 }
 
@@ -375,6 +432,109 @@ kvc_status kvc_gather(const kvc_params* params, const void* const* k, const void
   if (!k_out) { set_error("k_out is NULL"); return KVC_ERR_INVALID_ARG; }
   return launch_gather(pb, k, v, idx, lengths, offsets, total_budget, k_out, v_out, workspace,
                        static_cast<hipStream_t>(stream));
+}
+
+kvc_status kvc_cache_fill(const kvc_params* params, const void* const* k, const void* const* v, const int32_t* idx,
+                          const float* scores, const int32_t* lengths, const int64_t* offsets,
+                          const int64_t* cu_seqlens, int64_t total_budget, const kvc_cache* cache, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  Problem pb{};
+  CacheView c{};
+  kvc_status st = make_problem(params, cu_seqlens, &pb);
+  if (st != KVC_OK) return st;
+  if ((st = make_cache(params, cache, &c)) != KVC_OK) return st;
+  if ((st = check_ptr_table(k, pb.layers, "k")) != KVC_OK) return st;
+  if ((st = check_ptr_table(v, pb.layers, "v")) != KVC_OK) return st;
+  if (!lengths || !offsets) { set_error("lengths or offsets is NULL"); return KVC_ERR_INVALID_ARG; }
+  if (scores && !cache->weight) { set_error("scores need the cache's weight"); return KVC_ERR_INVALID_ARG; }
+  if (total_budget < 0 || total_budget > int64_t(pb.sel_rows) * pb.total) {
+    set_error("total_budget outside [0, rows*T]"); return KVC_ERR_INVALID_ARG;
+  }
+  const bool order = idx && pb.order == KVC_ORDER_POSITION;
+  if (order && (st = check_ws(workspace, workspace_bytes, gather_workspace_bytes(pb))) != KVC_OK) return st;
+  if (total_budget == 0) return KVC_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (order && (st = launch_order(pb, idx, lengths, workspace, s, &idx)) != KVC_OK) return st;
+  return launch_cache_fill(pb, k, v, idx, scores, lengths, offsets, total_budget, cache->format, c, s);
+}
+
+kvc_status kvc_cache_append(const kvc_params* params, int32_t layer, const void* k_new, const void* v_new,
+                            const int32_t* lengths, const kvc_cache* cache, void* stream) {
+  Problem pb{};
+  CacheView c{};
+  kvc_status st = make_cache_problem(params, cache, &pb, &c);
+  if (st != KVC_OK) return st;
+  if ((st = check_layer(pb, layer)) != KVC_OK) return st;
+  if (!k_new || !v_new || !lengths) { set_error("k_new, v_new or lengths is NULL"); return KVC_ERR_INVALID_ARG; }
+  return launch_cache_append(pb, layer, k_new, v_new, lengths, cache->format, c, static_cast<hipStream_t>(stream));
+}
+
+kvc_status kvc_cache_attend_workspace(const kvc_params* params, int64_t max_length, int32_t weights, size_t* bytes) {
+  kvc_status st = check_params(params);
+  if (st != KVC_OK) return st;
+  if (!bytes) { set_error("bytes is NULL"); return KVC_ERR_INVALID_ARG; }
+  if (max_length < 0 || max_length >= (int64_t(1) << 29)) {
+    set_error("max_length outside [0, 2^29)"); return KVC_ERR_INVALID_ARG;
+  }
+  Problem pb{};
+  describe(params, &pb);
+  *bytes = attend_workspace_bytes(pb, max_length, weights != 0);
+  return KVC_OK;
+}
+
+kvc_status kvc_cache_attend(const kvc_params* params, int32_t layer, const void* q, const int32_t* lengths,
+                            int64_t max_length, const kvc_cache* cache, void* out, float* lse,
+                            const float* weight_in, float* weight_out, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  Problem pb{};
+  CacheView c{};
+  kvc_status st = make_cache_problem(params, cache, &pb, &c);
+  if (st != KVC_OK) return st;
+  if ((st = check_layer(pb, layer)) != KVC_OK) return st;
+  if (max_length < 0) { set_error("max_length must be >= 0"); return KVC_ERR_INVALID_ARG; }
+  max_length = std::min(max_length, int64_t(cache->table_width) * KVC_BLOCK_TOKENS);
+  if (!q || !lengths || !out) { set_error("q, lengths or out is NULL"); return KVC_ERR_INVALID_ARG; }
+  if (weight_in && !weight_out) { set_error("weight_in without weight_out"); return KVC_ERR_INVALID_ARG; }
+  if (!attend_fits(pb, max_length, weight_out != nullptr)) {
+    set_error("hq * window * tokens too large for one call"); return KVC_ERR_UNSUPPORTED;
+  }
+  const size_t need = attend_workspace_bytes(pb, max_length, weight_out != nullptr);
+  if ((st = check_ws(workspace, workspace_bytes, need)) != KVC_OK) return st;
+  return launch_cache_attend(pb, layer, q, lengths, max_length, cache->format, c, out, lse, weight_in, weight_out,
+                             workspace, static_cast<hipStream_t>(stream));
+}
+
+kvc_status kvc_cache_evict_workspace(const kvc_params* params, int64_t max_keep, size_t* bytes) {
+  kvc_status st = check_params(params);
+  if (st != KVC_OK) return st;
+  if (!bytes) { set_error("bytes is NULL"); return KVC_ERR_INVALID_ARG; }
+  if (max_keep < 0 || max_keep >= (int64_t(1) << 29)) {
+    set_error("max_keep outside [0, 2^29)"); return KVC_ERR_INVALID_ARG;
+  }
+  Problem pb{};
+  describe(params, &pb);
+  *bytes = evict_workspace_bytes(pb, max_keep);
+  return KVC_OK;
+}
+
+kvc_status kvc_cache_evict(const kvc_params* params, const int32_t* lengths, const int32_t* keep, int64_t max_keep,
+                           const kvc_cache* cache, const int32_t* table_out, int32_t* lengths_out, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  Problem pb{};
+  CacheView c{};
+  kvc_status st = make_cache_problem(params, cache, &pb, &c);
+  if (st != KVC_OK) return st;
+  if (!cache->weight) { set_error("eviction needs the cache's weight"); return KVC_ERR_INVALID_ARG; }
+  if (!lengths || !keep || !table_out || !lengths_out) {
+    set_error("lengths, keep, table_out or lengths_out is NULL"); return KVC_ERR_INVALID_ARG;
+  }
+  if (table_out == cache->table || lengths_out == lengths) {
+    set_error("table_out and lengths_out must not be the inputs"); return KVC_ERR_INVALID_ARG;
+  }
+  if ((st = check_tokens("max_keep", max_keep, cache->table_width)) != KVC_OK) return st;
+  if ((st = check_ws(workspace, workspace_bytes, evict_workspace_bytes(pb, max_keep))) != KVC_OK) return st;
+  return launch_cache_evict(pb, lengths, keep, max_keep, cache->format, c, table_out, lengths_out, workspace,
+                            static_cast<hipStream_t>(stream));
 }
 
 kvc_status kvc_copy_probe(void* dst, const void* src, size_t bytes, void* stream) {

@@ -1,0 +1,510 @@
+// kvc_cache_attend: attention of M query tokens over the 8-bit block cache.
+//
+// Mathematics, per (sequence, KV head), rows r = (g, m) of the G query heads that share it:
+//   s[r,c] = scale * ks(block of c) * sum_d q[r,d] kc[c,d]        kc, vc: codes as numbers
+//   p[r,c] = 2^(s log2e - ref)                                      one pass, running reference and sum
+//   out[r,:] = sum_c p[r,c] vs(block) vc[c,:] / sum_c p[r,c]
+// Codes of both formats are bf16 numbers exactly, so both products run on the bf16 matrix cores with
+// fp32 accumulation; the scales are applied to the fp32 logits and to the fp32 probabilities
+// (exactly, they are powers of two).  bf16 calls round the probabilities to bf16 for the second product
+// (half a step, 2^-8 relative, which is what the output's own rounding costs); float32 calls split
+// queries and probabilities into three bf16 terms each, 24 bits, and lose nothing.
+//
+// Layout: v_mfma_f32_16x16x32_bf16 with tokens on the rows and queries on the columns of the first
+// product.  A wave takes a block of 64 tokens as four tiles; tile t holds the tokens 16*g + 4*t + i
+// (g, i: the lane group and register of the result), so that a lane ends up with the probabilities
+// of the 16 consecutive tokens of its group, in the order in which the second product wants them as
+// its operand, and with one query: the softmax needs two cross-lane steps per block and the probabilities
+// none.  The other operand, V transposed, is 16 consecutive bytes of a dimension's row of the block.
+// Nothing goes through LDS before the four waves of a workgroup join their results.
+//
+// Work is split over the tokens: a workgroup takes `chunk` blocks of one head (its waves every fourth
+// one); attend_join adds the splits of a row and, where weights are gathered, turns the stored
+// logits into probabilities once the sum over all tokens is known.
+#include <algorithm>
+#include <cmath>
+
+#include "kvc_cache.h"
+
+namespace kvc {
+
+namespace {
+
+constexpr int CA_THREADS = 256;
+constexpr int CA_WAVES = CA_THREADS / 64;
+// A reference further than this below the largest logit is moved up (log2 units): sums stay below
+// 2^8 * 2^30 and rescaling is rare.
+constexpr float CA_SLACK = 8.0f;
+
+struct AttendArgs {
+  const void* q;
+  void* out;
+  float* lse;               // may be null
+  const int32_t* lengths;
+  float* part_o;            // [batch * hkv * rows, splits, d]
+  float2* part_ml;          // [batch * hkv * rows, splits]: reference, sum
+  float* logits;            // [batch * hkv * rows, lpad] in log2 units, or null
+  const float* weight_in;   // may be null
+  float* weight_out;        // may be null
+  CacheView c;
+  int layer, group, window, rows, row_chunks, splits, chunk, max_length, lpad, causal;
+  float scale_log2;
+};
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Both halves / all four rows of 16 lanes see the combined value of lanes l, l^16, l^32, l^48.
+__device__ __forceinline__ float across_max(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float across_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Eight floats as TERMS bf16 vectors whose sum they are (to 8 bits a term).
+template <int TERMS>
+__device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8_t (&t)[TERMS]) {
+  float rest[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+  for (int n = 0; n < TERMS; ++n)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      t[n][i] = (__bf16)rest[i];
+      if (n + 1 < TERMS) rest[i] -= (float)t[n][i];
+    }
+}
+
+template <typename T> struct Store4;
+template <> struct Store4<float> {
+  static __device__ __forceinline__ void put(float* p, f32x4_t x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = x[i];
+  }
+};
+template <> struct Store4<uint16_t> {
+  static __device__ __forceinline__ void put(uint16_t* p, f32x4_t x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = __builtin_bit_cast(uint16_t, (__bf16)x[i]);
+  }
+};
+
+// Tokens of the row that this call reads.
+__device__ __forceinline__ int attend_length(const AttendArgs& a, int64_t row) {
+  return min(cache_length(a.c, a.lengths[row]), a.max_length);
+}
+
+// NJ: groups of 64 dimensions; QT: tiles of 16 query rows per workgroup.
+// grid: (splits * row_chunks * hkv, 1, batch), the head fastest: with 8 heads all row chunks of a head
+// run on the same chiplet and share its L2.
+template <int FMT, typename T, int NJ, int QT>
+__global__ __launch_bounds__(CA_THREADS, NJ <= 2 && QT == 1 && sizeof(T) == 2 ? 4 : NJ <= 2 || sizeof(T) == 2 ? 2 : 1)
+void attend_split(AttendArgs a) {
+  constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
+  constexpr int NT = 4 * NJ;                        // tiles of 16 dimensions
+  extern __shared__ __align__(16) float lds[];      // [waves][nq][d], nq = query rows of this workgroup
+  __shared__ float sm[CA_WAVES][16 * QT], sl[CA_WAVES][16 * QT];
+  const CacheView& c = a.c;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const int d = c.d, b = blockIdx.z;
+  const int x = blockIdx.x / c.hkv, h = blockIdx.x - x * c.hkv;
+  const int split = x / a.row_chunks, rc = x - split * a.row_chunks;
+  const int64_t row = cache_row(c, b, a.layer, h);
+  const int hh = cache_head(c, h);
+  const int len = attend_length(a, row);
+  const int nb = (len + CB_TOKENS - 1) / CB_TOKENS;
+  const int lo = split * a.chunk, hi = min(lo + a.chunk, nb);
+  if (split > 0 && lo >= nb) return;                // attend_join knows that this split is empty
+  const int r0 = rc * 16 * QT, nq = min(a.rows - r0, 16 * QT);
+  const int64_t out_row = ((int64_t)b * c.hkv + h) * a.rows + r0;
+
+  // ---- queries: lane col holds row col, dimensions 64 j + 16 g + 8 half ----
+  bf16x8_t q[QT][NJ][2][TERMS];
+  int limit[QT];                                    // tokens that the lane's query sees
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int r = t * 16 + col;
+    limit[t] = a.causal && r < nq ? len - (a.window - 1 - (r0 + r) % a.window) : len;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int at = 64 * j + 16 * g + 8 * half;
+        Row8<T> w;
+        w.clear();
+        if (r < nq && at < d) w.load(static_cast<const T*>(a.q) + (out_row + r) * d + at);
+        float f[8];
+        w.get(f);
+        split_terms<TERMS>(f, q[t][j][half]);
+      }
+  }
+  // offsets inside a block: K row of tile 0, V row of tile 0; pieces past d repeat ones that are there
+  // (their queries are zero, their results are not stored)
+  const int k_off = (16 * (col >> 2) + (col & 3)) * d;
+  int k_piece[NJ], v_off[NT];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) k_piece[j] = 64 * j + 16 * g < d ? 64 * j + 16 * g : 0;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) v_off[n] = min(16 * n, d - 16) * CB_TOKENS + col * CB_TOKENS + 16 * g;
+
+  f32x4_t o[QT][NT];
+  float ref[QT], sum[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    ref[t] = -INFINITY;
+    sum[t] = 0.f;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) o[t][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const size_t block_bytes = (size_t)CB_TOKENS * d;
+  int my_id = -1;
+  float my_ks = 0.f, my_vs = 0.f;
+  int it = 0;
+  for (int p = lo + wave; p < hi; p += CA_WAVES, ++it) {
+    if ((it & 63) == 0) {                           // the next 64 blocks of this wave, one per lane
+      const int pp = p + CA_WAVES * lane;
+      my_id = pp < hi ? c.table[row * c.width + pp] : -1;
+      if (my_id >= c.blocks) my_id = -1;
+      const size_t at = (size_t)max(my_id, 0) * c.hb + hh;
+      my_ks = c.k_scale[at];
+      my_vs = c.v_scale[at];
+    }
+    const int id = __builtin_amdgcn_readlane(my_id, it & 63);
+    float* lrow = a.logits ? a.logits + (size_t)p * CB_TOKENS + 16 * g : nullptr;
+    if (id < 0) {                                   // an entry that names no block: its tokens are absent
+      if (a.logits)
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+          if (t * 16 + col < nq)
+            for (int i = 0; i < 16; ++i) lrow[(size_t)(out_row + t * 16 + col) * a.lpad + i] = -INFINITY;
+      continue;
+    }
+    const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_ks), it & 63)) * a.scale_log2;
+    const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_vs), it & 63));
+    const uint8_t* kb = c.k + ((size_t)id * c.hb + hh) * block_bytes;
+    const uint8_t* vb = c.v + ((size_t)id * c.hb + hh) * block_bytes;
+    u32x4_t kw[4][NJ], vw[NT];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        kw[t][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(kb + k_off + 4 * t * d + k_piece[j]));
+#pragma unroll
+    for (int n = 0; n < NT; ++n) vw[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vb + v_off[n]));
+
+    // ---- logits ----
+    f32x4_t s[QT][4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) s[qt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const bf16x8_t kf = Code<FMT>::widen(kw[t][j][2 * half], kw[t][j][2 * half + 1]);
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+            for (int n = TERMS - 1; n >= 0; --n)
+              s[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[qt][j][half][n], s[qt][t], 0, 0, 0);
+        }
+    }
+    const int first = p * CB_TOKENS + 16 * g;       // the lane's 16 tokens
+    const bool tail = (p + 1) * CB_TOKENS > len - (a.causal ? a.window - 1 : 0);   // wave-uniform
+    bf16x8_t pf[QT][2][TERMS];
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[qt][t] *= ks;
+      if (tail)
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (first + 4 * t + i >= limit[qt]) s[qt][t][i] = -INFINITY;
+      if (a.logits && qt * 16 + col < nq) {
+        float* to = lrow + (size_t)(out_row + qt * 16 + col) * a.lpad;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4_t*>(to + 4 * t) = s[qt][t];
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[qt][t][i]);
+      top = across_max(top);
+      if (__ballot(top > ref[qt] + CA_SLACK)) {
+        const float to = fmaxf(ref[qt], top);
+        const float f = ref[qt] == -INFINITY ? 0.f : exp2_fast(ref[qt] - to);   // 0: nothing summed yet
+        ref[qt] = to;
+        sum[qt] *= f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[qt][n] *= f;
+      }
+      const float base = ref[qt] == -INFINITY ? 0.f : ref[qt];   // no token seen yet: 2^(-inf - 0) = 0
+      float pr[2][8];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = exp2_fast(s[qt][t][i] - base);
+          sum[qt] += e;
+          pr[t >> 1][4 * (t & 1) + i] = e * vs;
+        }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) split_terms<TERMS>(pr[u], pf[qt][u]);
+    }
+    // ---- values ----
+    const bool ragged = (p + 1) * CB_TOKENS > len;  // slots behind the last token hold anything
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if (ragged) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int left = len - first - 4 * w;     // tokens of this word that are there
+          vw[n][w] = left >= 4 ? vw[n][w] : left <= 0 ? 0u : vw[n][w] & ((1u << (8 * left)) - 1);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8_t vf = Code<FMT>::widen(vw[n][2 * u], vw[n][2 * u + 1]);
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+          for (int m = TERMS - 1; m >= 0; --m)
+            o[qt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt][u][m], o[qt][n], 0, 0, 0);
+      }
+    }
+  }
+
+  // ---- join the waves ----
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    sum[qt] = across_sum(sum[qt]);
+    if (g == 0) { sm[wave][qt * 16 + col] = ref[qt]; sl[wave][qt * 16 + col] = sum[qt]; }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    const int r = qt * 16 + col;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < CA_WAVES; ++w) top = fmaxf(top, sm[w][r]);
+    const float f = ref[qt] == -INFINITY ? 0.f : exp2_fast(ref[qt] - top);
+    if (r < nq)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        if (16 * n < d) *reinterpret_cast<f32x4_t*>(lds + ((size_t)wave * nq + r) * d + 16 * n + 4 * g) = o[qt][n] * f;
+  }
+  __syncthreads();
+  const bool whole = a.splits == 1;
+  for (int e = tid; e < nq * d / 4; e += CA_THREADS) {
+    const int r = e / (d / 4), at = (e - r * (d / 4)) * 4;
+    float top = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int w = 0; w < CA_WAVES; ++w) top = fmaxf(top, sm[w][r]);
+#pragma unroll
+    for (int w = 0; w < CA_WAVES; ++w) total += sm[w][r] == -INFINITY ? 0.f : sl[w][r] * exp2_fast(sm[w][r] - top);
+    f32x4_t y{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < CA_WAVES; ++w) y += *reinterpret_cast<const f32x4_t*>(lds + ((size_t)w * nq + r) * d + at);
+    if (whole) {
+      const float inv = total > 0.f ? 1.0f / total : 0.f;        // a query that sees no token: zeros
+      Store4<T>::put(static_cast<T*>(a.out) + (out_row + r) * d + at, y * inv);
+      if (at == 0 && a.lse) a.lse[out_row + r] = total > 0.f ? (top + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+    } else {
+      *reinterpret_cast<f32x4_t*>(a.part_o + ((out_row + r) * a.splits + split) * d + at) = y;
+    }
+    if (at == 0 && a.part_ml) a.part_ml[(out_row + r) * a.splits + split] = make_float2(top, total);
+  }
+}
+
+// Reference and sum of a row over its first n splits, by one wave.
+__device__ __forceinline__ float2 join_sums(const float2* __restrict__ ml, int n, int lane) {
+  float top = -INFINITY, total = 0.f;
+  for (int s = lane; s < n; s += 64) top = fmaxf(top, ml[s].x);
+  top = wave_max(top);
+  for (int s = lane; s < n; s += 64) total += ml[s].x == -INFINITY ? 0.f : ml[s].y * exp2_fast(ml[s].x - top);
+#pragma unroll
+  for (int off = 32; off; off >>= 1) total += __shfl_xor(total, off);
+  return make_float2(top, total);
+}
+
+// The first `joins` workgroups: one wave per query row adds its splits.  The others: 64 * CJ_BLOCKS
+// tokens of one head each, whose gathered weight grows by the probabilities of the head's rows.
+constexpr int CJ_BLOCKS = CA_THREADS / CB_TOKENS;
+constexpr int CJ_ROWS = 64;                         // rows whose log-sum-exps are in LDS at a time
+template <typename T>
+__global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t joins, int weight_chunks, int batch) {
+  __shared__ float lse2[CJ_ROWS];
+  const CacheView& c = a.c;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, d = c.d;
+  if (blockIdx.x < joins) {
+    const int64_t r = (int64_t)blockIdx.x * CA_WAVES + wave;
+    if (r >= (int64_t)batch * c.hkv * a.rows) return;
+    const int64_t bh = r / a.rows;
+    const int b = (int)(bh / c.hkv), h = (int)(bh - (int64_t)b * c.hkv);
+    const int nb = (attend_length(a, cache_row(c, b, a.layer, h)) + CB_TOKENS - 1) / CB_TOKENS;
+    const int n = max((nb + a.chunk - 1) / a.chunk, 1);
+    const float2* ml = a.part_ml + r * a.splits;
+    const float2 all = join_sums(ml, n, lane);
+    f32x4_t y{0.f, 0.f, 0.f, 0.f};
+    const int at = lane * 4;
+    const bool on = at < d;
+    for (int s0 = 0; s0 < n; s0 += 64) {
+      const float m = s0 + lane < n ? ml[s0 + lane].x : -INFINITY;
+      const float f = m == -INFINITY ? 0.f : exp2_fast(m - all.x);
+      const int most = min(n - s0, 64);
+      const float* from = a.part_o + (r * a.splits + s0) * d + at;
+#pragma unroll 8
+      for (int s = 0; s < most; ++s) {
+        const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
+        if (on) y += *reinterpret_cast<const f32x4_t*>(from + (size_t)s * d) * fs;
+      }
+    }
+    const float inv = all.y > 0.f ? 1.0f / all.y : 0.f;
+    if (on) Store4<T>::put(static_cast<T*>(a.out) + r * d + at, y * inv);
+    if (lane == 0 && a.lse) a.lse[r] = all.y > 0.f ? (all.x + __builtin_amdgcn_logf(all.y)) * 0.6931471805599453f : -INFINITY;
+    return;
+  }
+  const int64_t w = blockIdx.x - joins;
+  const int64_t bh = w / weight_chunks;
+  const int chunk = (int)(w - bh * weight_chunks);
+  const int b = (int)(bh / c.hkv), h = (int)(bh - (int64_t)b * c.hkv);
+  const int64_t row = cache_row(c, b, a.layer, h);
+  const int len = attend_length(a, row);
+  const int token = chunk * CA_THREADS + tid;
+  if (chunk * CA_THREADS >= len) return;            // uniform
+  const int n = max(((len + CB_TOKENS - 1) / CB_TOKENS + a.chunk - 1) / a.chunk, 1);
+  const int id = token < len ? c.table[row * c.width + token / CB_TOKENS] : -1;
+  const bool on = id >= 0 && id < c.blocks;
+  const size_t at = ((size_t)(on ? id : 0) * c.hb + cache_head(c, h)) * CB_TOKENS + token % CB_TOKENS;
+  float gained = on && a.weight_in ? a.weight_in[at] : 0.f;
+  for (int r0 = 0; r0 < a.rows; r0 += CJ_ROWS) {
+    const int most = min(a.rows - r0, CJ_ROWS);
+    for (int r = wave; r < most; r += CA_WAVES) {
+      const float2 all = join_sums(a.part_ml + (bh * a.rows + r0 + r) * a.splits, n, lane);
+      // a row that sees no token adds nothing: 2^(-inf - inf)
+      if (lane == 0) lse2[r] = all.y > 0.f ? all.x + __builtin_amdgcn_logf(all.y) : INFINITY;
+    }
+    __syncthreads();
+    if (on)
+      for (int r = 0; r < most; ++r)
+        gained += exp2_fast(a.logits[(size_t)(bh * a.rows + r0 + r) * a.lpad + token] - lse2[r]);
+    __syncthreads();
+  }
+  if (on) a.weight_out[at] = gained;
+}
+
+// How a call is split.  Enough workgroups that every compute unit has a few, but no chunk below one block
+// per wave.  The workspace is that of the most splits that any shorter max_length asks for.
+struct AttendPlan {
+  int rows, qt, row_chunks, chunk, splits, lpad;
+  size_t off_o, off_ml, off_logits, total;
+};
+
+AttendPlan attend_plan(const Problem& pb, int64_t max_length, bool weights) {
+  AttendPlan P{};
+  P.rows = pb.group * pb.window;
+  P.qt = P.rows > 16 && pb.d <= 128 ? 2 : 1;
+  P.row_chunks = (P.rows + 16 * P.qt - 1) / (16 * P.qt);
+  const int64_t nb = std::max<int64_t>((max_length + CB_TOKENS - 1) / CB_TOKENS, 1);
+  const int64_t heads = int64_t(pb.batch) * pb.hkv * P.row_chunks;
+  const int64_t want = std::max<int64_t>(1024 / heads, 1);       // splits of a head
+  const int64_t chunk = std::max<int64_t>((nb + want - 1) / want, CA_WAVES);
+  P.chunk = int((chunk + CA_WAVES - 1) / CA_WAVES * CA_WAVES);
+  P.splits = int((nb + P.chunk - 1) / P.chunk);
+  P.lpad = int(nb * CB_TOKENS);
+  const size_t all = size_t(pb.batch) * pb.hkv * P.rows;
+  const size_t most = size_t(std::min(want, (nb + CA_WAVES - 1) / CA_WAVES));   // >= splits, and never falls with nb
+  size_t cur = 0;
+  P.off_o = cur;
+  if (most > 1) cur += align_up(all * most * pb.d * 4);
+  P.off_ml = cur;
+  if (most > 1 || weights) cur += align_up(all * most * 8);
+  P.off_logits = cur;
+  if (weights) cur += align_up(all * size_t(P.lpad) * 4);
+  P.total = cur;
+  return P;
+}
+
+template <int FMT, typename T>
+kvc_status attend_form(const Problem& pb, const AttendPlan& P, const AttendArgs& a, unsigned grid, hipStream_t stream) {
+  const dim3 g(grid, 1, pb.batch);
+  const size_t lds = size_t(CA_WAVES) * std::min(P.rows, 16 * P.qt) * pb.d * 4;
+#define KVC_ATTEND(NJ, QT)                                                                                \
+  KVC_LAUNCH("attend_split", stream, attend_split<FMT, T, NJ, QT><<<g, CA_THREADS, lds, stream>>>(a))
+  const int nj = (pb.d + 63) / 64;
+  if (P.qt == 2) {
+    if (nj == 1) KVC_ATTEND(1, 2); else KVC_ATTEND(2, 2);
+  } else {
+    if (nj == 1) KVC_ATTEND(1, 1);
+    else if (nj == 2) KVC_ATTEND(2, 1);
+    else if (nj == 3) KVC_ATTEND(3, 1);
+    else KVC_ATTEND(4, 1);
+  }
+#undef KVC_ATTEND
+  return KVC_OK;
+}
+
+}  // namespace
+
+size_t attend_workspace_bytes(const Problem& pb, int64_t max_length, bool weights) {
+  return attend_plan(pb, max_length, weights).total;
+}
+
+// Workgroups of the two launches; a launch holds fewer than 2^24 of them.
+bool attend_fits(const Problem& pb, int64_t max_length, bool weights) {
+  const AttendPlan P = attend_plan(pb, max_length, weights);
+  const int64_t split = int64_t(P.splits) * P.row_chunks * pb.hkv;
+  const int64_t heads = int64_t(pb.batch) * pb.hkv;
+  const int64_t join = (heads * P.rows + CA_WAVES - 1) / CA_WAVES + (weights ? heads * ((max_length + CA_THREADS - 1) / CA_THREADS) : 0);
+  return split < (1 << 24) && join < (1 << 24);
+}
+
+kvc_status launch_cache_attend(const Problem& pb, int layer, const void* q, const int32_t* lengths, int64_t max_length,
+                               int format, const CacheView& c, void* out, float* lse, const float* weight_in,
+                               float* weight_out, void* ws, hipStream_t stream) {
+  const bool weights = weight_out != nullptr;
+  const AttendPlan P = attend_plan(pb, max_length, weights);
+  char* base = static_cast<char*>(ws);
+  AttendArgs a{};
+  a.q = q; a.out = out; a.lse = lse; a.lengths = lengths;
+  a.part_o = reinterpret_cast<float*>(base + P.off_o);
+  a.part_ml = P.splits > 1 || weights ? reinterpret_cast<float2*>(base + P.off_ml) : nullptr;
+  a.logits = weights ? reinterpret_cast<float*>(base + P.off_logits) : nullptr;
+  a.weight_in = weight_in; a.weight_out = weight_out;
+  a.c = c;
+  a.layer = layer; a.group = pb.group; a.window = pb.window; a.rows = P.rows; a.row_chunks = P.row_chunks;
+  a.splits = P.splits; a.chunk = P.chunk; a.max_length = int(max_length); a.lpad = P.lpad; a.causal = pb.causal_tail;
+  a.scale_log2 = pb.scale * 1.4426950408889634f;
+  const unsigned grid = unsigned(P.splits) * P.row_chunks * pb.hkv;
+  const bool half = pb.dtype == KVC_BF16;
+  kvc_status st;
+  if (format == KVC_E4M3)
+    st = half ? attend_form<KVC_E4M3, uint16_t>(pb, P, a, grid, stream) : attend_form<KVC_E4M3, float>(pb, P, a, grid, stream);
+  else
+    st = half ? attend_form<KVC_INT8, uint16_t>(pb, P, a, grid, stream) : attend_form<KVC_INT8, float>(pb, P, a, grid, stream);
+  if (st != KVC_OK) return st;
+  const int64_t heads = int64_t(pb.batch) * pb.hkv;
+  const int64_t joins = P.splits > 1 ? (heads * P.rows + CA_WAVES - 1) / CA_WAVES : 0;
+  const int chunks = int((max_length + CA_THREADS - 1) / CA_THREADS);
+  const int64_t total = joins + (weights ? heads * chunks : 0);
+  if (total == 0) return KVC_OK;
+#define KVC_JOIN(T) \
+  KVC_LAUNCH("attend_join", stream, attend_join<T><<<(unsigned)total, CA_THREADS, 0, stream>>>(a, joins, std::max(chunks, 1), pb.batch))
+  if (half) KVC_JOIN(uint16_t); else KVC_JOIN(float);
+#undef KVC_JOIN
+  return KVC_OK;
+}
+
+}  // namespace kvc

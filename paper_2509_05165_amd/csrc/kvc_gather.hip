@@ -318,6 +318,30 @@ static GatherLayout gather_layout(const Problem& pb) {
 
 size_t gather_workspace_bytes(const Problem& pb) { return gather_layout(pb).total; }
 
+kvc_status launch_order(const Problem& pb, const int32_t* idx, const int32_t* lengths, void* ws, hipStream_t stream,
+                        const int32_t** ordered) {
+  const int hpb = pb.unstructured ? 1 : pb.hkv;
+  const GatherLayout G = gather_layout(pb);
+  int32_t* sel = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + G.off_sel);
+  uint32_t* mask = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + G.off_mask);
+  const int lh = pb.layers * pb.hkv;
+  const size_t words_all = size_t(lh) * G.words;
+  if (pb.max_seqlen <= ORDER_LDS_TOKENS) {
+    const size_t lds = size_t((pb.max_seqlen + 31) / 32) * 4;
+    KVC_LAUNCH("order_list", stream, order_list<<<dim3(lh, pb.batch), 1024, lds, stream>>>(
+        idx, lengths, pb.seq, pb.layers, pb.hkv, hpb, int(pb.total), sel));
+  } else {
+    dim3 gm((unsigned)((pb.max_seqlen + 255) / 256), lh, pb.batch);
+    KVC_LAUNCH("order_clear", stream, order_clear<<<1024, 256, 0, stream>>>(mask, words_all));
+    KVC_LAUNCH("order_mark", stream, order_mark<<<gm, 256, 0, stream>>>(
+        idx, lengths, pb.seq, pb.layers, pb.hkv, hpb, int(pb.total), G.words, mask));
+    KVC_LAUNCH("order_compact", stream, order_compact<<<dim3(lh, pb.batch), 1024, 0, stream>>>(
+        mask, pb.seq, int(pb.total), G.words, sel));
+  }
+  *ordered = sel;
+  return KVC_OK;
+}
+
 kvc_status launch_gather(const Problem& pb, const void* const* k, const void* const* v,
                          const int32_t* idx, const int32_t* lengths, const int64_t* offsets,
                          int64_t total_budget, void* k_out, void* v_out, void* ws,
@@ -328,24 +352,8 @@ kvc_status launch_gather(const Problem& pb, const void* const* k, const void* co
   const int hpb = pb.unstructured ? 1 : pb.hkv;
   const int64_t pool_rows = total_budget * hpb;
   if (pb.order == KVC_ORDER_POSITION && pb.total > 0) {
-    const GatherLayout G = gather_layout(pb);
-    int32_t* sel = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + G.off_sel);
-    uint32_t* mask = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + G.off_mask);
-    const int lh = pb.layers * pb.hkv;
-    const size_t words_all = size_t(lh) * G.words;
-    if (pb.max_seqlen <= ORDER_LDS_TOKENS) {
-      const size_t lds = size_t((pb.max_seqlen + 31) / 32) * 4;
-      KVC_LAUNCH("order_list", stream, order_list<<<dim3(lh, pb.batch), 1024, lds, stream>>>(
-          idx, lengths, pb.seq, pb.layers, pb.hkv, hpb, int(pb.total), sel));
-    } else {
-      dim3 gm((unsigned)((pb.max_seqlen + 255) / 256), lh, pb.batch);
-      KVC_LAUNCH("order_clear", stream, order_clear<<<1024, 256, 0, stream>>>(mask, words_all));
-      KVC_LAUNCH("order_mark", stream, order_mark<<<gm, 256, 0, stream>>>(
-          idx, lengths, pb.seq, pb.layers, pb.hkv, hpb, int(pb.total), G.words, mask));
-      KVC_LAUNCH("order_compact", stream, order_compact<<<dim3(lh, pb.batch), 1024, 0, stream>>>(
-          mask, pb.seq, int(pb.total), G.words, sel));
-    }
-    idx = sel;
+    kvc_status st = launch_order(pb, idx, lengths, ws, stream, &idx);
+    if (st != KVC_OK) return st;
   }
   int wave_rows = 64;
   while (wave_rows > 16 && pool_rows < int64_t(GA_WAVES) * wave_rows) wave_rows /= 2;

@@ -95,6 +95,27 @@ kvc_status launch_gather(const Problem& pb, const void* const* k, const void* co
                          int64_t total_budget, void* k_out, void* v_out, void* ws,
                          hipStream_t stream);
 
+// Position order: the retained prefixes of idx as ascending lists in ws (gather_workspace_bytes).
+kvc_status launch_order(const Problem& pb, const int32_t* idx, const int32_t* lengths, void* ws, hipStream_t stream,
+                        const int32_t** ordered);
+
+// The 8-bit block cache (kvc_cache.h).  pb of the last three has no sequence table.
+struct CacheView;
+kvc_status launch_cache_fill(const Problem& pb, const void* const* k, const void* const* v, const int32_t* idx,
+                             const float* scores, const int32_t* lengths, const int64_t* offsets, int64_t total_budget,
+                             int format, const CacheView& c, hipStream_t stream);
+kvc_status launch_cache_append(const Problem& pb, int layer, const void* k_new, const void* v_new, const int32_t* lengths,
+                               int format, const CacheView& c, hipStream_t stream);
+size_t attend_workspace_bytes(const Problem& pb, int64_t max_length, bool weights);
+bool attend_fits(const Problem& pb, int64_t max_length, bool weights);
+kvc_status launch_cache_attend(const Problem& pb, int layer, const void* q, const int32_t* lengths, int64_t max_length,
+                               int format, const CacheView& c, void* out, float* lse, const float* weight_in,
+                               float* weight_out, void* ws, hipStream_t stream);
+size_t evict_workspace_bytes(const Problem& pb, int64_t max_keep);
+kvc_status launch_cache_evict(const Problem& pb, const int32_t* lengths, const int32_t* keep, int64_t max_keep, int format,
+                              const CacheView& c, const int32_t* table_out, int32_t* lengths_out, void* ws,
+                              hipStream_t stream);
+
 kvc_status launch_copy_probe(void* dst, const void* src, size_t bytes, hipStream_t stream);
 kvc_status launch_mfma_probe(const void* operands, int iterations, int mode, float* sink,
                              int64_t* cycles, double* flops, hipStream_t stream);
