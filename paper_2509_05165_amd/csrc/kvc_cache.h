@@ -95,7 +95,10 @@ template <> struct Code<KVC_INT8> {
     const float a = (float)(int8_t)(w >> (8 * i)), b = (float)(int8_t)(w >> (8 * i + 8));
     return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
   }
+  // (The words are opaque: else codes that a loop carries from one turn to the next are carried as four
+  // registers of one byte each.)
   static __device__ __forceinline__ bf16x8_t widen(uint32_t a, uint32_t b) {
+    asm("" : "+v"(a), "+v"(b));
     return __builtin_bit_cast(bf16x8_t, u32x4_t{pair(a, 0), pair(a, 2), pair(b, 0), pair(b, 2)});
   }
 };

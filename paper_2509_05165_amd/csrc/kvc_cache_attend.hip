@@ -96,24 +96,63 @@ template <> struct Store4<uint16_t> {
   }
 };
 
+// Waves per SIMD that the registers of a form are held to: one block of K and V (32 registers per 64
+// dimensions), the queries and the output have to fit.  More waves would not help (they only spread the
+// loads over more of the pool): 128 dimensions, bf16, 1 x 128k tokens of 8 heads 55.9 us with two, 67.8
+// with three (and a few spilled registers).
+constexpr int attend_waves(int nj, int qt, int esz) {
+  return esz == 2 ? (nj == 1 && qt == 1 ? 3 : nj <= 3 ? 2 : 1) : (nj <= 2 && qt == 1 ? 2 : 1);
+}
+
+// 16 bytes of codes.  Codes that one workgroup alone reads carry the streaming hint (with whole lines,
+// see PAIRED): 16 x 400..13000 tokens of 8 heads 47.6 us without, 39.2 with; 1 x 128k 55.9 / 48.2.
+template <bool STREAM>
+__device__ __forceinline__ u32x4_t load16(const uint8_t* p) {
+  const u32x4_t* q = reinterpret_cast<const u32x4_t*>(p);
+  return STREAM ? __builtin_nontemporal_load(q) : *q;
+}
+constexpr int DPP_ROR8 = 0x128;                     // rotate rows of 16 lanes by eight
+
 // Tokens of the row that this call reads.
 __device__ __forceinline__ int attend_length(const AttendArgs& a, int64_t row) {
   return min(cache_length(a.c, a.lengths[row]), a.max_length);
 }
 
-// NJ: groups of 64 dimensions; QT: tiles of 16 query rows per workgroup.
+// The blocks of a wave: their ids and scales, 64 at a time in the lanes of three registers.
+struct BlockList {
+  int ids;
+  float ks, vs;
+  // p: block of lane 0; lane i holds block p + CA_WAVES * i
+  __device__ __forceinline__ void load(const AttendArgs& a, int64_t row, int hh, int p, int hi, int lane) {
+    const int at = p + CA_WAVES * lane;
+    ids = at < hi ? a.c.table[row * a.c.width + at] : -1;
+    if (ids >= a.c.blocks) ids = -1;
+    const size_t s = (size_t)max(ids, 0) * a.c.hb + hh;
+    ks = a.c.k_scale[s];
+    vs = a.c.v_scale[s];
+  }
+  __device__ __forceinline__ int id(int i) const { return __builtin_amdgcn_readlane(ids, i & 63); }
+  static __device__ __forceinline__ float lane_of(float x, int i) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i & 63));
+  }
+};
+
+// NJ: groups of 64 dimensions, d = 64 * NJ where EXACT; QT: tiles of 16 query rows per workgroup.
 // grid: (splits * row_chunks * hkv, 1, batch), the head fastest: with 8 heads all row chunks of a head
 // run on the same chiplet and share its L2.
-template <int FMT, typename T, int NJ, int QT>
-__global__ __launch_bounds__(CA_THREADS, NJ <= 2 && QT == 1 && sizeof(T) == 2 ? 4 : NJ <= 2 || sizeof(T) == 2 ? 2 : 1)
-void attend_split(AttendArgs a) {
+//
+// Bound by HBM: 2 * 64 * d bytes of codes per block and head.  A wave keeps one block of K and one of V
+// in flight: the next block's K is asked for as soon as this block's logits are there, the next V as soon
+// as this block's output is.
+template <int FMT, typename T, int NJ, bool EXACT, int QT, bool STREAM>
+__global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void attend_split(AttendArgs a) {
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
   constexpr int NT = 4 * NJ;                        // tiles of 16 dimensions
   extern __shared__ __align__(16) float lds[];      // [waves][nq][d], nq = query rows of this workgroup
   __shared__ float sm[CA_WAVES][16 * QT], sl[CA_WAVES][16 * QT];
   const CacheView& c = a.c;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
-  const int d = c.d, b = blockIdx.z;
+  const int d = EXACT ? 64 * NJ : c.d, b = blockIdx.z;
   const int x = blockIdx.x / c.hkv, h = blockIdx.x - x * c.hkv;
   const int split = x / a.row_chunks, rc = x - split * a.row_chunks;
   const int64_t row = cache_row(c, b, a.layer, h);
@@ -122,8 +161,52 @@ void attend_split(AttendArgs a) {
   const int nb = (len + CB_TOKENS - 1) / CB_TOKENS;
   const int lo = split * a.chunk, hi = min(lo + a.chunk, nb);
   if (split > 0 && lo >= nb) return;                // attend_join knows that this split is empty
+  const int first_block = lo + __builtin_amdgcn_readfirstlane(wave);
+  BlockList list;
+  list.load(a, row, hh, first_block, hi, lane);
   const int r0 = rc * 16 * QT, nq = min(a.rows - r0, 16 * QT);
   const int64_t out_row = ((int64_t)b * c.hkv + h) * a.rows + r0;
+
+  // Offsets inside a block: K row of tile 0, V row of tile 0.  Pieces past d repeat ones that are there
+  // (their queries are zero, their results are not stored).
+  // PAIRED: a load takes whole lines of 128 bytes of eight rows instead of half lines of sixteen, the second
+  // one the other eight rows; exchanging the upper and lower lanes of the two gives the operands (operand()).
+  constexpr bool PAIRED = EXACT && NJ % 2 == 0;
+  uint32_t k_off[NJ], v_off[NT];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int piece = 64 * j + 16 * g;
+    if (PAIRED) k_off[j] = (16 * (col >> 2 & 1) + (col & 3) + 32 * (j & 1)) * d + 128 * (j >> 1) + 64 * (col >> 3) + 16 * g;
+    else k_off[j] = (16 * (col >> 2) + (col & 3)) * d + (EXACT || piece < d ? piece : 0);
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) v_off[n] = (EXACT ? 16 * n : min(16 * n, d - 16)) * CB_TOKENS + col * CB_TOKENS + 16 * g;
+  const uint32_t block_bytes = CB_TOKENS * d;
+  u32x4_t kw[4][NJ], vw[NT];
+  const auto load_k = [&](int id) {                 // an entry that names no block: any block, masked below
+    const uint8_t* kb = c.k + ((size_t)max(id, 0) * c.hb + hh) * block_bytes;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) kw[t][j] = load16<STREAM && (PAIRED || NJ == 1)>(kb + k_off[j] + uint32_t(4 * t * d));
+  };
+  const auto load_v = [&](int id) {
+    const uint8_t* vb = c.v + ((size_t)max(id, 0) * c.hb + hh) * block_bytes;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) vw[n] = load16<STREAM>(vb + v_off[n]);
+  };
+  // word w of the 16 bytes of tile t and dimensions 64 j + 16 g
+  const auto operand = [&](int t, int j, int w) -> uint32_t {
+    if (!PAIRED) return kw[t][j][w];
+    const int even = (int)kw[t][j & ~1][w], odd = (int)kw[t][j | 1][w];
+    return (uint32_t)(j & 1 ? __builtin_amdgcn_update_dpp(odd, even, DPP_ROR8, 0xf, 0x3, false)
+                            : __builtin_amdgcn_update_dpp(even, odd, DPP_ROR8, 0xf, 0xc, false));
+  };
+  if (first_block < hi) {
+    const int id = list.id(0);
+    load_k(id);
+    load_v(id);
+  }
 
   // ---- queries: lane col holds row col, dimensions 64 j + 16 g + 8 half ----
   bf16x8_t q[QT][NJ][2][TERMS];
@@ -145,14 +228,6 @@ void attend_split(AttendArgs a) {
         split_terms<TERMS>(f, q[t][j][half]);
       }
   }
-  // offsets inside a block: K row of tile 0, V row of tile 0; pieces past d repeat ones that are there
-  // (their queries are zero, their results are not stored)
-  const int k_off = (16 * (col >> 2) + (col & 3)) * d;
-  int k_piece[NJ], v_off[NT];
-#pragma unroll
-  for (int j = 0; j < NJ; ++j) k_piece[j] = 64 * j + 16 * g < d ? 64 * j + 16 * g : 0;
-#pragma unroll
-  for (int n = 0; n < NT; ++n) v_off[n] = min(16 * n, d - 16) * CB_TOKENS + col * CB_TOKENS + 16 * g;
 
   f32x4_t o[QT][NT];
   float ref[QT], sum[QT];
@@ -164,84 +239,62 @@ void attend_split(AttendArgs a) {
     for (int n = 0; n < NT; ++n) o[t][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  const size_t block_bytes = (size_t)CB_TOKENS * d;
-  int my_id = -1;
-  float my_ks = 0.f, my_vs = 0.f;
   int it = 0;
-  for (int p = lo + wave; p < hi; p += CA_WAVES, ++it) {
-    if ((it & 63) == 0) {                           // the next 64 blocks of this wave, one per lane
-      const int pp = p + CA_WAVES * lane;
-      my_id = pp < hi ? c.table[row * c.width + pp] : -1;
-      if (my_id >= c.blocks) my_id = -1;
-      const size_t at = (size_t)max(my_id, 0) * c.hb + hh;
-      my_ks = c.k_scale[at];
-      my_vs = c.v_scale[at];
-    }
-    const int id = __builtin_amdgcn_readlane(my_id, it & 63);
-    float* lrow = a.logits ? a.logits + (size_t)p * CB_TOKENS + 16 * g : nullptr;
-    if (id < 0) {                                   // an entry that names no block: its tokens are absent
-      if (a.logits)
-#pragma unroll
-        for (int t = 0; t < QT; ++t)
-          if (t * 16 + col < nq)
-            for (int i = 0; i < 16; ++i) lrow[(size_t)(out_row + t * 16 + col) * a.lpad + i] = -INFINITY;
-      continue;
-    }
-    const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_ks), it & 63)) * a.scale_log2;
-    const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_vs), it & 63));
-    const uint8_t* kb = c.k + ((size_t)id * c.hb + hh) * block_bytes;
-    const uint8_t* vb = c.v + ((size_t)id * c.hb + hh) * block_bytes;
-    u32x4_t kw[4][NJ], vw[NT];
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-        kw[t][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(kb + k_off + 4 * t * d + k_piece[j]));
-#pragma unroll
-    for (int n = 0; n < NT; ++n) vw[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vb + v_off[n]));
+  for (int p = first_block; p < hi; p += CA_WAVES, ++it) {
+    const int id = list.id(it);
+    const float ks = BlockList::lane_of(list.ks, it) * a.scale_log2, vs = BlockList::lane_of(list.vs, it);
+    const bool more = p + CA_WAVES < hi;
+    if (more && ((it + 1) & 63) == 0) list.load(a, row, hh, p + CA_WAVES, hi, lane);
+    const int next = list.id(it + 1);
 
     // ---- logits ----
     f32x4_t s[QT][4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt) s[qt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < 4; ++t) s[qt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < NJ; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const bf16x8_t kf = Code<FMT>::widen(kw[t][j][2 * half], kw[t][j][2 * half + 1]);
+      for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const bf16x8_t kf = Code<FMT>::widen(operand(t, j, 2 * half), operand(t, j, 2 * half + 1));
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
             for (int n = TERMS - 1; n >= 0; --n)
               s[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[qt][j][half][n], s[qt][t], 0, 0, 0);
         }
-    }
+        __builtin_amdgcn_sched_barrier(0);          // no more than one step's widened codes in registers
+      }
+    if (more) load_k(next);
+    const int here = id < 0 ? 0 : len;              // tokens of an absent block are masked like those past the end
     const int first = p * CB_TOKENS + 16 * g;       // the lane's 16 tokens
-    const bool tail = (p + 1) * CB_TOKENS > len - (a.causal ? a.window - 1 : 0);   // wave-uniform
+    const bool tail = (p + 1) * CB_TOKENS > here - (a.causal ? a.window - 1 : 0);   // wave-uniform
+    const float shift = __builtin_amdgcn_logf(vs);  // whole: vs is a power of two
+    const float inv_vs = inverse_scale(vs);
     bf16x8_t pf[QT][2][TERMS];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t) s[qt][t] *= ks;
-      if (tail)
+      if (tail) {
+        const int seen = min(limit[qt], here);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (first + 4 * t + i >= limit[qt]) s[qt][t][i] = -INFINITY;
+          for (int i = 0; i < 4; ++i) s[qt][t][i] = first + 4 * t + i < seen ? s[qt][t][i] : -INFINITY;
+      }
       if (a.logits && qt * 16 + col < nq) {
-        float* to = lrow + (size_t)(out_row + qt * 16 + col) * a.lpad;
+        float* to = a.logits + (size_t)(out_row + qt * 16 + col) * a.lpad + first;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4_t*>(to + 4 * t) = s[qt][t];
+        for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4_t*>(to + 4 * t) = s[qt][t] * ks;
       }
       float top = -INFINITY;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[qt][t][i]);
-      top = across_max(top);
+      top = across_max(top) * ks;                   // ks > 0
       if (__ballot(top > ref[qt] + CA_SLACK)) {
         const float to = fmaxf(ref[qt], top);
         const float f = ref[qt] == -INFINITY ? 0.f : exp2_fast(ref[qt] - to);   // 0: nothing summed yet
@@ -250,40 +303,44 @@ void attend_split(AttendArgs a) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) o[qt][n] *= f;
       }
-      const float base = ref[qt] == -INFINITY ? 0.f : ref[qt];   // no token seen yet: 2^(-inf - 0) = 0
-      float pr[2][8];
+      // p * vs = 2^(s ks - ref + log2 vs); no token seen yet: 2^(-inf - 0) = 0
+      const float base = shift - (ref[qt] == -INFINITY ? 0.f : ref[qt]);
+      float pr[2][8], part = 0.f;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float e = exp2_fast(s[qt][t][i] - base);
-          sum[qt] += e;
-          pr[t >> 1][4 * (t & 1) + i] = e * vs;
+          const float e = exp2_fast(fmaf(s[qt][t][i], ks, base));
+          part += e;
+          pr[t >> 1][4 * (t & 1) + i] = e;
         }
+      sum[qt] = fmaf(part, inv_vs, sum[qt]);
 #pragma unroll
       for (int u = 0; u < 2; ++u) split_terms<TERMS>(pr[u], pf[qt][u]);
     }
     // ---- values ----
-    const bool ragged = (p + 1) * CB_TOKENS > len;  // slots behind the last token hold anything
+    if ((p + 1) * CB_TOKENS > here) {               // slots behind the last token hold anything: no code 0 times NaN
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      if (ragged) {
+      for (int w = 0; w < 4; ++w) {
+        const int left = here - first - 4 * w;      // tokens of this word that are there
+        const uint32_t mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const int left = len - first - 4 * w;     // tokens of this word that are there
-          vw[n][w] = left >= 4 ? vw[n][w] : left <= 0 ? 0u : vw[n][w] & ((1u << (8 * left)) - 1);
-        }
+        for (int n = 0; n < NT; ++n) vw[n][w] &= mask;
       }
+    }
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
         const bf16x8_t vf = Code<FMT>::widen(vw[n][2 * u], vw[n][2 * u + 1]);
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
           for (int m = TERMS - 1; m >= 0; --m)
             o[qt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt][u][m], o[qt][n], 0, 0, 0);
+        if (n % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
-    }
+    if (more) load_v(next);
   }
 
   // ---- join the waves ----
@@ -339,41 +396,46 @@ __device__ __forceinline__ float2 join_sums(const float2* __restrict__ ml, int n
   return make_float2(top, total);
 }
 
-// The first `joins` workgroups: one wave per query row adds its splits.  The others: 64 * CJ_BLOCKS
-// tokens of one head each, whose gathered weight grows by the probabilities of the head's rows.
-constexpr int CJ_BLOCKS = CA_THREADS / CB_TOKENS;
+// The first `joins` workgroups add the splits of a query row each: groups of d / 4 lanes take every
+// groups-th split, four dimensions a lane.  The others: CJ_TOKENS tokens of one head each, whose gathered
+// weight grows by the probabilities of the head's rows; the logits of the next CJ_AHEAD rows are always
+// in flight, the first ones while the log-sum-exps are worked out.
 constexpr int CJ_ROWS = 64;                         // rows whose log-sum-exps are in LDS at a time
+constexpr int CJ_TOKENS = CA_THREADS * 4;
+constexpr int CJ_AHEAD = 4;
+static_assert(CJ_ROWS % CJ_AHEAD == 0, "the rows ahead are those of the next turn");
 template <typename T>
-__global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t joins, int weight_chunks, int batch) {
+__global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t joins, int weight_chunks) {
   __shared__ float lse2[CJ_ROWS];
+  __shared__ __align__(16) float acc[CA_THREADS * 4];
   const CacheView& c = a.c;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, d = c.d;
   if (blockIdx.x < joins) {
-    const int64_t r = (int64_t)blockIdx.x * CA_WAVES + wave;
-    if (r >= (int64_t)batch * c.hkv * a.rows) return;
+    const int64_t r = blockIdx.x;
     const int64_t bh = r / a.rows;
     const int b = (int)(bh / c.hkv), h = (int)(bh - (int64_t)b * c.hkv);
     const int nb = (attend_length(a, cache_row(c, b, a.layer, h)) + CB_TOKENS - 1) / CB_TOKENS;
     const int n = max((nb + a.chunk - 1) / a.chunk, 1);
     const float2* ml = a.part_ml + r * a.splits;
     const float2 all = join_sums(ml, n, lane);
+    const int wide = d / 4, groups = CA_THREADS / wide, group = tid / wide, at = (tid - group * wide) * 4;
+    const float* from = a.part_o + r * a.splits * d + at;
     f32x4_t y{0.f, 0.f, 0.f, 0.f};
-    const int at = lane * 4;
-    const bool on = at < d;
-    for (int s0 = 0; s0 < n; s0 += 64) {
-      const float m = s0 + lane < n ? ml[s0 + lane].x : -INFINITY;
-      const float f = m == -INFINITY ? 0.f : exp2_fast(m - all.x);
-      const int most = min(n - s0, 64);
-      const float* from = a.part_o + (r * a.splits + s0) * d + at;
-#pragma unroll 8
-      for (int s = 0; s < most; ++s) {
-        const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
-        if (on) y += *reinterpret_cast<const f32x4_t*>(from + (size_t)s * d) * fs;
+    if (group < groups)
+#pragma unroll 4
+      for (int s = group; s < n; s += groups) {
+        const float m = ml[s].x;
+        const f32x4_t o = *reinterpret_cast<const f32x4_t*>(from + (size_t)s * d);
+        y += o * (m == -INFINITY ? 0.f : exp2_fast(m - all.x));
       }
+    *reinterpret_cast<f32x4_t*>(acc + tid * 4) = y;
+    __syncthreads();
+    if (group == 0) {
+      for (int i = 1; i < min(groups, n); ++i) y += *reinterpret_cast<const f32x4_t*>(acc + (i * wide + tid) * 4);
+      const float inv = all.y > 0.f ? 1.0f / all.y : 0.f;
+      Store4<T>::put(static_cast<T*>(a.out) + r * d + at, y * inv);
     }
-    const float inv = all.y > 0.f ? 1.0f / all.y : 0.f;
-    if (on) Store4<T>::put(static_cast<T*>(a.out) + r * d + at, y * inv);
-    if (lane == 0 && a.lse) a.lse[r] = all.y > 0.f ? (all.x + __builtin_amdgcn_logf(all.y)) * 0.6931471805599453f : -INFINITY;
+    if (tid == 0 && a.lse) a.lse[r] = all.y > 0.f ? (all.x + __builtin_amdgcn_logf(all.y)) * 0.6931471805599453f : -INFINITY;
     return;
   }
   const int64_t w = blockIdx.x - joins;
@@ -382,13 +444,19 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
   const int b = (int)(bh / c.hkv), h = (int)(bh - (int64_t)b * c.hkv);
   const int64_t row = cache_row(c, b, a.layer, h);
   const int len = attend_length(a, row);
-  const int token = chunk * CA_THREADS + tid;
-  if (chunk * CA_THREADS >= len) return;            // uniform
+  if (chunk * CJ_TOKENS >= len) return;             // uniform
+  const int token = chunk * CJ_TOKENS + tid * 4;    // four tokens of one block
   const int n = max(((len + CB_TOKENS - 1) / CB_TOKENS + a.chunk - 1) / a.chunk, 1);
   const int id = token < len ? c.table[row * c.width + token / CB_TOKENS] : -1;
   const bool on = id >= 0 && id < c.blocks;
+  const float* from = a.logits + (size_t)(bh * a.rows) * a.lpad + (on ? token : 0);
+  f32x4_t s[CJ_AHEAD];
+#pragma unroll
+  for (int i = 0; i < CJ_AHEAD; ++i) s[i] = *reinterpret_cast<const f32x4_t*>(from + (size_t)min(i, a.rows - 1) * a.lpad);
   const size_t at = ((size_t)(on ? id : 0) * c.hb + cache_head(c, h)) * CB_TOKENS + token % CB_TOKENS;
-  float gained = on && a.weight_in ? a.weight_in[at] : 0.f;
+  u32x4_word w_in{0, 0, 0, 0};
+  if (on && a.weight_in) w_in = *reinterpret_cast<const u32x4_word*>(a.weight_in + at);
+  float gained[4] = {0.f, 0.f, 0.f, 0.f};
   for (int r0 = 0; r0 < a.rows; r0 += CJ_ROWS) {
     const int most = min(a.rows - r0, CJ_ROWS);
     for (int r = wave; r < most; r += CA_WAVES) {
@@ -397,12 +465,32 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
       if (lane == 0) lse2[r] = all.y > 0.f ? all.x + __builtin_amdgcn_logf(all.y) : INFINITY;
     }
     __syncthreads();
-    if (on)
-      for (int r = 0; r < most; ++r)
-        gained += exp2_fast(a.logits[(size_t)(bh * a.rows + r0 + r) * a.lpad + token] - lse2[r]);
+    for (int r = 0; r < most; r += CJ_AHEAD) {
+      f32x4_t now[CJ_AHEAD];
+#pragma unroll
+      for (int i = 0; i < CJ_AHEAD; ++i) now[i] = s[i];
+      if (r0 + r + CJ_AHEAD < a.rows)
+#pragma unroll
+        for (int i = 0; i < CJ_AHEAD; ++i)
+          s[i] = *reinterpret_cast<const f32x4_t*>(from + (size_t)min(r0 + r + CJ_AHEAD + i, a.rows - 1) * a.lpad);
+#pragma unroll
+      for (int i = 0; i < CJ_AHEAD; ++i)
+        if (r + i < most) {
+          const float m = lse2[r + i];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) gained[e] += exp2_fast(now[i][e] - m);
+        }
+    }
     __syncthreads();
   }
-  if (on) a.weight_out[at] = gained;
+  if (!on) return;
+  u32x4_word y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = __float_as_uint(__uint_as_float(w_in[e]) + gained[e]);
+  float* to = a.weight_out + at;
+  if (token + 4 <= len) *reinterpret_cast<u32x4_word*>(to) = y;
+  else
+    for (int e = 0; e < len - token; ++e) to[e] = __uint_as_float(y[e]);
 }
 
 // How a call is split.  Enough workgroups that every compute unit has a few, but no chunk below one block
@@ -419,7 +507,7 @@ AttendPlan attend_plan(const Problem& pb, int64_t max_length, bool weights) {
   P.row_chunks = (P.rows + 16 * P.qt - 1) / (16 * P.qt);
   const int64_t nb = std::max<int64_t>((max_length + CB_TOKENS - 1) / CB_TOKENS, 1);
   const int64_t heads = int64_t(pb.batch) * pb.hkv * P.row_chunks;
-  const int64_t want = std::max<int64_t>(1024 / heads, 1);       // splits of a head
+  const int64_t want = std::max<int64_t>(1536 / heads, 1);       // splits of a head
   const int64_t chunk = std::max<int64_t>((nb + want - 1) / want, CA_WAVES);
   P.chunk = int((chunk + CA_WAVES - 1) / CA_WAVES * CA_WAVES);
   P.splits = int((nb + P.chunk - 1) / P.chunk);
@@ -441,16 +529,23 @@ template <int FMT, typename T>
 kvc_status attend_form(const Problem& pb, const AttendPlan& P, const AttendArgs& a, unsigned grid, hipStream_t stream) {
   const dim3 g(grid, 1, pb.batch);
   const size_t lds = size_t(CA_WAVES) * std::min(P.rows, 16 * P.qt) * pb.d * 4;
-#define KVC_ATTEND(NJ, QT)                                                                                \
-  KVC_LAUNCH("attend_split", stream, attend_split<FMT, T, NJ, QT><<<g, CA_THREADS, lds, stream>>>(a))
+#define KVC_ATTEND(NJ, QT, STREAM)                                                                                        \
+  do {                                                                                                                    \
+    if (pb.d == 64 * NJ)                                                                                                  \
+      KVC_LAUNCH("attend_split", stream, attend_split<FMT, T, NJ, true, QT, STREAM><<<g, CA_THREADS, lds, stream>>>(a));  \
+    else                                                                                                                  \
+      KVC_LAUNCH("attend_split", stream, attend_split<FMT, T, NJ, false, QT, STREAM><<<g, CA_THREADS, lds, stream>>>(a)); \
+  } while (0)
   const int nj = (pb.d + 63) / 64;
   if (P.qt == 2) {
-    if (nj == 1) KVC_ATTEND(1, 2); else KVC_ATTEND(2, 2);
-  } else {
-    if (nj == 1) KVC_ATTEND(1, 1);
-    else if (nj == 2) KVC_ATTEND(2, 1);
-    else if (nj == 3) KVC_ATTEND(3, 1);
-    else KVC_ATTEND(4, 1);
+    if (nj == 1) KVC_ATTEND(1, 2, false); else KVC_ATTEND(2, 2, false);
+  } else if (P.row_chunks == 1) {
+    if (nj == 1) KVC_ATTEND(1, 1, true);
+    else if (nj == 2) KVC_ATTEND(2, 1, true);
+    else if (nj == 3) KVC_ATTEND(3, 1, true);
+    else KVC_ATTEND(4, 1, true);
+  } else {                                          // d > 128: row chunks read the same codes
+    if (nj == 3) KVC_ATTEND(3, 1, false); else KVC_ATTEND(4, 1, false);
   }
 #undef KVC_ATTEND
   return KVC_OK;
@@ -467,7 +562,7 @@ bool attend_fits(const Problem& pb, int64_t max_length, bool weights) {
   const AttendPlan P = attend_plan(pb, max_length, weights);
   const int64_t split = int64_t(P.splits) * P.row_chunks * pb.hkv;
   const int64_t heads = int64_t(pb.batch) * pb.hkv;
-  const int64_t join = (heads * P.rows + CA_WAVES - 1) / CA_WAVES + (weights ? heads * ((max_length + CA_THREADS - 1) / CA_THREADS) : 0);
+  const int64_t join = heads * P.rows + (weights ? heads * ((max_length + CJ_TOKENS - 1) / CJ_TOKENS) : 0);
   return split < (1 << 24) && join < (1 << 24);
 }
 
@@ -496,12 +591,12 @@ kvc_status launch_cache_attend(const Problem& pb, int layer, const void* q, cons
     st = half ? attend_form<KVC_INT8, uint16_t>(pb, P, a, grid, stream) : attend_form<KVC_INT8, float>(pb, P, a, grid, stream);
   if (st != KVC_OK) return st;
   const int64_t heads = int64_t(pb.batch) * pb.hkv;
-  const int64_t joins = P.splits > 1 ? (heads * P.rows + CA_WAVES - 1) / CA_WAVES : 0;
-  const int chunks = int((max_length + CA_THREADS - 1) / CA_THREADS);
+  const int64_t joins = P.splits > 1 ? heads * P.rows : 0;
+  const int chunks = int((max_length + CJ_TOKENS - 1) / CJ_TOKENS);
   const int64_t total = joins + (weights ? heads * chunks : 0);
   if (total == 0) return KVC_OK;
 #define KVC_JOIN(T) \
-  KVC_LAUNCH("attend_join", stream, attend_join<T><<<(unsigned)total, CA_THREADS, 0, stream>>>(a, joins, std::max(chunks, 1), pb.batch))
+  KVC_LAUNCH("attend_join", stream, attend_join<T><<<(unsigned)total, CA_THREADS, 0, stream>>>(a, joins, std::max(chunks, 1)))
   if (half) KVC_JOIN(uint16_t); else KVC_JOIN(float);
 #undef KVC_JOIN
   return KVC_OK;
