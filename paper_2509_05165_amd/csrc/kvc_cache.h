@@ -126,6 +126,10 @@ template <> struct Row8<uint16_t> {
   u32x4_any w;
   __device__ __forceinline__ void load(const uint16_t* p) { w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p)); }
   __device__ __forceinline__ void clear() { w = u32x4_any{0, 0, 0, 0}; }
+  __device__ __forceinline__ void opaque() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { uint32_t x = w[i]; asm("" : "+v"(x)); w[i] = x; }
+  }
   __device__ __forceinline__ void get(float (&x)[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -141,6 +145,7 @@ template <> struct Row8<float> {
     w[1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_word*>(p) + 1);
   }
   __device__ __forceinline__ void clear() { w[0] = w[1] = u32x4_word{0, 0, 0, 0}; }
+  __device__ __forceinline__ void opaque() {}       // already floats
   __device__ __forceinline__ void get(float (&x)[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { x[i] = __uint_as_float(w[0][i]); x[4 + i] = __uint_as_float(w[1][i]); }

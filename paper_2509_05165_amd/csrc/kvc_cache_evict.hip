@@ -41,10 +41,10 @@ __device__ __forceinline__ int kept_tokens(const EvictArgs& a, int64_t row, int 
 // KPT > 0: every key of the row lies in registers, token i * EV_THREADS + tid in key[i].  KPT = 0: longer rows
 // read their weights again in every pass.
 template <int KPT>
-__global__ __launch_bounds__(EV_THREADS) void evict_select(EvictArgs a) {
+__global__ __launch_bounds__(EV_THREADS, KPT > 0 && KPT <= 16 ? 8 : 4) void evict_select(EvictArgs a) {
   __shared__ uint32_t hist[EV_BINS];
   __shared__ uint32_t part[EV_WAVES], found[2];
-  __shared__ uint32_t counts[2][2][EV_WAVES];
+  __shared__ uint32_t counts[KPT > 0 ? KPT * EV_WAVES : 2 * EV_WAVES];   // above | equal << 16 of a wave's 64 tokens
   const CacheView& c = a.c;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   for (int64_t head = blockIdx.x; head < a.heads; head += gridDim.x) {
@@ -59,19 +59,21 @@ __global__ __launch_bounds__(EV_THREADS) void evict_select(EvictArgs a) {
       continue;
     }
     if (keep == 0) continue;
-    const auto read = [&](int t) -> uint32_t {
-      if (t < a.keep_first || t >= len - a.keep_last) return EV_FORCED;
-      const int id = c.table[row * c.width + t / CB_TOKENS];
-      if (id < 0 || id >= c.blocks) return EV_ABSENT;
-      return float_to_ordered(c.weight[((size_t)id * c.hb + hh) * CB_TOKENS + t % CB_TOKENS]);
+    // key of token i * EV_THREADS + tid: a wave's 64 tokens are one block, whose id is a scalar
+    const int wave_s = __builtin_amdgcn_readfirstlane(wave);
+    const auto read = [&](int i) -> uint32_t {
+      const int block = i * EV_WAVES + wave_s, t = block * CB_TOKENS + lane;
+      if (block * CB_TOKENS >= len) return 0u;      // 0: no token; every token has a larger key
+      const int id = c.table[row * c.width + block];
+      const bool there = id >= 0 && id < c.blocks;
+      const uint32_t k = float_to_ordered(c.weight[((size_t)(there ? id : 0) * c.hb + hh) * CB_TOKENS + lane]);
+      const uint32_t key = t < a.keep_first || t >= len - a.keep_last ? EV_FORCED : there ? max(k, 1u) : EV_ABSENT;
+      return t < len ? key : 0u;
     };
     uint32_t key[KPT > 0 ? KPT : 1];
     if (KPT > 0)
 #pragma unroll
-      for (int i = 0; i < KPT; ++i) {
-        const int t = i * EV_THREADS + tid;
-        key[i] = t < len ? read(t) : 0u;
-      }
+      for (int i = 0; i < KPT; ++i) key[i] = read(i);
     const int chunks = (len + EV_THREADS - 1) / EV_THREADS;
 
     // ---- the keep-th largest key, digit by digit ----
@@ -81,17 +83,14 @@ __global__ __launch_bounds__(EV_THREADS) void evict_select(EvictArgs a) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
       for (int i = tid; i < EV_BINS; i += EV_THREADS) hist[i] = 0;
       __syncthreads();
-      const auto count = [&](uint32_t k, int t) {
-        if (t < len && (k & mask) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
+      const auto count = [&](uint32_t k) {
+        if (pass == 0 ? k != 0 : (k & mask) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
       };
       if (KPT > 0) {
 #pragma unroll
-        for (int i = 0; i < KPT; ++i) count(key[i], i * EV_THREADS + tid);
+        for (int i = 0; i < KPT; ++i) count(key[i]);
       } else {
-        for (int i = 0; i < chunks; ++i) {
-          const int t = i * EV_THREADS + tid;
-          if (t < len) count(read(t), t);
-        }
+        for (int i = 0; i < chunks; ++i) count(read(i));
       }
       __syncthreads();
       // thread tid holds the bins 2 tid and 2 tid + 1 counted from the top
@@ -118,54 +117,135 @@ __global__ __launch_bounds__(EV_THREADS) void evict_select(EvictArgs a) {
     }
 
     // ---- kept positions, ascending ----
-    uint32_t above = 0, equal = 0;                  // so far, of all earlier chunks
-    const auto emit = [&](int i, uint32_t k) {
-      const int t = i * EV_THREADS + tid;
-      const bool gt = t < len && k > prefix, eq = t < len && k == prefix;
-      const uint64_t bg = __ballot(gt), be = __ballot(eq);
-      uint32_t (*cnt)[EV_WAVES] = counts[i & 1];
-      if (lane == 0) { cnt[0][wave] = __popcll(bg); cnt[1][wave] = __popcll(be); }
-      __syncthreads();
-      uint32_t g0 = above, e0 = equal;
-#pragma unroll
-      for (int w = 0; w < EV_WAVES; ++w) {
-        const uint32_t x = cnt[0][w], y = cnt[1][w];
-        if (w < wave) { g0 += x; e0 += y; }
-        above += x;
-        equal += y;
+    // base: keys above and equal to the threshold in front of the wave's 64 tokens
+    const auto put = [&](int t, uint32_t k, uint32_t above, uint32_t equal) {
+      const bool gt = k > prefix;
+      const uint64_t bg = __ballot(gt), be = __ballot(k == prefix);
+      above = __builtin_amdgcn_mbcnt_hi((uint32_t)(bg >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bg, above));
+      bool take = gt;
+      if (be) {                                     // uniform: the few waves that hold the threshold itself
+        equal = __builtin_amdgcn_mbcnt_hi((uint32_t)(be >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)be, equal));
+        take = gt || (k == prefix && equal < left);
       }
-      const uint64_t below = (1ull << lane) - 1;
-      g0 += __popcll(bg & below);
-      e0 += __popcll(be & below);
-      const uint32_t at = g0 + min(e0, left);
-      if ((gt || (eq && e0 < left)) && at < (uint32_t)keep) list[at] = t;
+      const uint32_t at = above + min(equal, left);
+      if (take && at < (uint32_t)keep) list[at] = t;
     };
     if (KPT > 0) {
 #pragma unroll
-      for (int i = 0; i < KPT; ++i)
-        if (i < chunks) emit(i, key[i]);
+      for (int i = 0; i < KPT; ++i) {
+        const uint64_t gt = __ballot(key[i] > prefix), eq = __ballot(key[i] == prefix);
+        if (lane == 0) counts[i * EV_WAVES + wave] = __popcll(gt) | __popcll(eq) << 16;
+      }
+      __syncthreads();
+      if (wave == 0) {                              // exclusive sums over KPT * 16 entries, KPT / 4 per lane
+        constexpr int PER = KPT > 0 ? KPT / 4 : 1;
+        uint32_t mine[PER], incl = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) { mine[i] = counts[lane * PER + i]; incl += mine[i]; }
+        uint32_t run = incl;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+          const uint32_t o = __shfl_up(incl, off);
+          if (lane >= off) incl += o;
+        }
+        run = incl - run;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) { counts[lane * PER + i] = run; run += mine[i]; }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < KPT; ++i) {
+        const uint32_t base = counts[i * EV_WAVES + wave];
+        put(i * EV_THREADS + tid, key[i], base & 0xffff, base >> 16);
+      }
     } else {
+      uint32_t above = 0, equal = 0;                // of all earlier chunks
       for (int i = 0; i < chunks; ++i) {
         const int t = i * EV_THREADS + tid;
-        emit(i, t < len ? read(t) : 0u);
+        const uint32_t k = read(i);
+        const uint64_t gt = __ballot(k > prefix), eq = __ballot(k == prefix);
+        uint32_t* cnt = counts + (i & 1) * EV_WAVES;
+        if (lane == 0) cnt[wave] = __popcll(gt) | __popcll(eq) << 16;
+        __syncthreads();
+        uint32_t all = 0, before = 0;
+#pragma unroll
+        for (int w = 0; w < EV_WAVES; ++w) {
+          if (w < wave) before += cnt[w];
+          all += cnt[w];
+        }
+        put(t, k, above + (before & 0xffff), equal + (before >> 16));
+        above += all & 0xffff;
+        equal += all >> 16;
       }
     }
     __syncthreads();                                // shared memory is free for the next head
   }
 }
 
-// NU: 16-byte pieces of K per thread, 64 * d / 16 / 256 rounded up; ND: words of four dimensions of V per
-// thread, d / 16 rounded up.  V lies dimension by dimension, so a token of it is a column of bytes: lane =
-// token, and a wave reads the same dimension of its 64 tokens, neighbours in one or a few rows.
-template <int FMT, int NU, int ND>
-__global__ __launch_bounds__(EM_THREADS) void evict_move(EvictArgs a, int blocks, int64_t units) {
-  extern __shared__ __align__(16) uint8_t tile[];   // V codes [64][d + 4]
-  __shared__ float red[2 * EM_THREADS / 64];
+// One workgroup per block that is written, of one wave per 64 dimensions; K and V in launches of their
+// own (in one they share the registers of the larger: 1504 us instead of 367 + 601 for 105k blocks of
+// 64 x 128 int8 at half of their rows).  Every lane = token of the block first finds out where its token lies and
+// under which scale.
+//
+// K: a row of d bytes per token, moved as 16-byte pieces that stay in registers until the new scale is known.
+// V lies dimension by dimension: a token of it is a column of bytes.  A source block comes in whole, in lines,
+// and turns in LDS so that a lane holds the 64 bytes of one dimension.  Which of them stay is a scalar: two
+// v_perm per word put its kept bytes behind those that wait for a full word, which goes to the lane's
+// row in LDS.  (Measured on 105k blocks of 128 x 64, V alone: a byte at a time from source blocks in LDS
+// 1858 us; a branch per token 1344; the 64 bytes of a lane loaded by the lane itself, in pieces 64 bytes apart
+// over the wave, 1363.)  Rows whose scale the new block keeps are copied; only the others are decoded and rounded
+// again.
+constexpr int EM_STAGE = CB_TOKENS * 64;            // bytes of a wave's 64 dimensions of a source block
+constexpr int EM_ROW = CB_TOKENS / 4 + 1;           // words of a row that is written: 64 lanes lie in 64 different banks
+constexpr int EM_WAVE_LDS = EM_STAGE + 64 * EM_ROW * 4;
+
+__device__ __forceinline__ float move_max(float x, float* red, int waves) {
+  x = wave_max(x);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+  for (int i = 0; i < waves; ++i) x = fmaxf(x, red[i]);
+  return x;
+}
+
+// old over new scale: a code that is not 0 has at most 2^18 of it, a larger one belongs to a row of zeros
+__device__ __forceinline__ float move_ratio(float old_scale, float inverse) { return fminf(old_scale * inverse, EM_RATIO); }
+
+template <int FMT>
+__device__ __forceinline__ float largest_code(uint32_t w, float most) {
+  float x[4];
+  Code<FMT>::decode(w, x);
+  return fmaxf(fmaxf(fmaxf(fmaxf(most, fabsf(x[0])), fabsf(x[1])), fabsf(x[2])), fabsf(x[3]));
+}
+template <int FMT>
+__device__ __forceinline__ uint32_t rescale(uint32_t w, float a, float b, float c, float d) {
+  float x[4];
+  asm("" : "+v"(w));                                // else the numbers of the maximum are kept in registers until here
+  Code<FMT>::decode(w, x);
+  return Code<FMT>::encode(x[0] * a, x[1] * b, x[2] * c, x[3] * d);
+}
+__device__ __forceinline__ float lane_float(float x, int lane) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
+}
+
+// blockDim: 64 * waves, waves = d / 64 rounded up.  magic: 65536 / (d / 16) rounded up.  VALUES: V, else K.
+// Bound by HBM: K 4.9 TB/s, V 4.7 TB/s of the bytes that it moves, which are those of every source block that
+// a kept token lies in.
+template <int FMT, bool VALUES>
+__global__ __launch_bounds__(EM_THREADS) void evict_move(EvictArgs a, int blocks, int64_t units, uint32_t magic) {
+  extern __shared__ __align__(16) uint8_t smem[];   // EM_WAVE_LDS per wave
+  __shared__ float red[EM_THREADS / 64];
   const CacheView& c = a.c;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, d = c.d, pieces = d / 16, stride = d + 4;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int64_t head = u / blocks;
-    const int j = (int)(u - head * blocks);
+  const int tid = threadIdx.x, lane = tid & 63, d = c.d, pieces = d / 16, waves = blockDim.x / 64;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // workgroups go to the eight chiplets in turn: each is given EM_STRETCH neighbours, which share source blocks
+  // of V, at a time
+  constexpr int EM_STRETCH = 32;
+  for (int64_t x = blockIdx.x; x < (units + 8 * EM_STRETCH - 1) / (8 * EM_STRETCH) * (8 * EM_STRETCH); x += gridDim.x) {
+    const int in = (int)(x & (8 * EM_STRETCH - 1));
+    const int64_t w = x - in + (in & 7) * EM_STRETCH + (in >> 3);
+    if (w >= units) continue;
+    const int64_t head = w / blocks;
+    const int j = (int)(w - head * blocks);
     const int64_t row = head / c.hb;
     const int hh = (int)(head - row * c.hb);
     const int keep = kept_tokens(a, row, cache_length(c, a.lengths[row]));
@@ -173,114 +253,182 @@ __global__ __launch_bounds__(EM_THREADS) void evict_move(EvictArgs a, int blocks
     const int to = a.table_out[row * c.width + j];
     if (to < 0 || to >= c.blocks) continue;
     const int here = min(keep - j * CB_TOKENS, CB_TOKENS);
-    const int32_t* list = a.list + head * a.lpad + j * CB_TOKENS;
     const int32_t* ids = c.table + row * c.width;
-
-    u32x4_t kw[NU];
-    float kf[NU];
-#pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      const int e = i * EM_THREADS + tid, token = e / pieces, piece = e - token * pieces;
-      kw[i] = u32x4_t{0, 0, 0, 0};
-      kf[i] = 0.f;
-      if (token < here) {
-        const int p = list[token], id = ids[p / CB_TOKENS];
-        if (id >= 0 && id < c.blocks) {
-          const size_t at = (size_t)id * c.hb + hh;
-          kf[i] = c.k_scale[at];
-          kw[i] = *reinterpret_cast<const u32x4_t*>(c.k + (at * CB_TOKENS + p % CB_TOKENS) * d + piece * 16);
-        }
-      }
-    }
-    uint32_t vw[ND];
-    float vf = 0.f, wt = 0.f;
-    const uint8_t* from = nullptr;
-    if (lane < here) {
-      const int p = list[lane], id = ids[p / CB_TOKENS];
-      if (id >= 0 && id < c.blocks) {
-        const size_t at = (size_t)id * c.hb + hh;
-        vf = c.v_scale[at];
-        wt = c.weight[at * CB_TOKENS + p % CB_TOKENS];
-        from = c.v + at * CB_TOKENS * d + p % CB_TOKENS;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < ND; ++i) {
-      const int dim = (i * 4 + wave) * 4;
-      vw[i] = 0;
-      if (from && dim < d)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) vw[i] |= (uint32_t)from[(dim + q) * CB_TOKENS] << (8 * q);
-    }
-    float ka = 0.f, va = 0.f;
-#pragma unroll
-    for (int i = 0; i < NU; ++i)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        float x[4];
-        Code<FMT>::decode(kw[i][w], x);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) ka = fmaxf(ka, fabsf(x[e]) * kf[i]);
-      }
-#pragma unroll
-    for (int i = 0; i < ND; ++i) {
-      float x[4];
-      Code<FMT>::decode(vw[i], x);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) va = fmaxf(va, fabsf(x[e]) * vf);
-    }
-    ka = wave_max(ka);
-    va = wave_max(va);
-    if (lane == 0) { red[2 * wave] = ka; red[2 * wave + 1] = va; }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < EM_THREADS / 64; ++i) { ka = fmaxf(ka, red[2 * i]); va = fmaxf(va, red[2 * i + 1]); }
-    const float ks = block_scale<FMT>(ka), vs = block_scale<FMT>(va);
-    // old over new scale: a code that is not 0 has at most 2^18 of it, a larger one belongs to a row of zeros
-    const float ki = inverse_scale(ks), vi = fminf(vf * inverse_scale(vs), EM_RATIO);
     const size_t at = (size_t)to * c.hb + hh;
-    uint8_t* ko = c.k + at * CB_TOKENS * d;
-    uint8_t* vo = c.v + at * CB_TOKENS * d;
+
+    // lane = token, the same in every wave; scale 0: not there
+    int page = 1 << 30, slot = 0, id = -1;
+    float old_scale = 0.f, weight = 0.f;
+    if (lane < here) {
+      const int p = a.list[head * a.lpad + j * CB_TOKENS + lane];
+      page = p / CB_TOKENS;
+      slot = p % CB_TOKENS;
+      id = ids[page];
+      if (id >= c.blocks) id = -1;
+      if (id >= 0) {
+        const size_t from = (size_t)id * c.hb + hh;
+        old_scale = (VALUES ? c.v_scale : c.k_scale)[from];
+        if (VALUES && wave == 0) weight = c.weight[from * CB_TOKENS + slot];
+      }
+    }
+
+    if constexpr (!VALUES) {
+      u32x4_t kw[4];
+      float kf[4], most = 0.f;
 #pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      const int e = i * EM_THREADS + tid;
-      if (e < CB_TOKENS * pieces) {
-        const float f = fminf(kf[i] * ki, EM_RATIO);
-        u32x4_t w4;
+      for (int i = 0; i < 4; ++i) {
+        const int e = i * blockDim.x + tid;
+        const int token = min((int)(e * magic >> 16), CB_TOKENS - 1), piece = e - token * pieces;
+        const int from_id = __shfl(id, token), from_slot = __shfl(slot, token);
+        kf[i] = __shfl(old_scale, token);
+        kw[i] = u32x4_t{0, 0, 0, 0};
+        if (e < CB_TOKENS * pieces && from_id >= 0)
+          kw[i] = *reinterpret_cast<const u32x4_t*>(c.k + (((size_t)from_id * c.hb + hh) * CB_TOKENS + from_slot) * d + piece * 16);
+      }
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          float x[4];
-          Code<FMT>::decode(kw[i][w], x);
-          w4[w] = Code<FMT>::encode(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+      for (int i = 0; i < 4; ++i) {
+        float code = 0.f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) code = largest_code<FMT>(kw[i][q], code);
+        most = fmaxf(most, code * kf[i]);
+      }
+      const float scale = block_scale<FMT>(move_max(most, red, waves)), inv = inverse_scale(scale);
+      uint8_t* ko = c.k + at * CB_TOKENS * d;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int e = i * blockDim.x + tid;
+        if (__ballot(kf[i] != scale)) {
+          const float f = move_ratio(kf[i], inv);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) kw[i][q] = rescale<FMT>(kw[i][q], f, f, f, f);
         }
-        *reinterpret_cast<u32x4_t*>(ko + (size_t)e * 16) = w4;
+        if (e < CB_TOKENS * pieces) __builtin_nontemporal_store(kw[i], reinterpret_cast<u32x4_t*>(ko + (size_t)e * 16));
       }
-    }
+      if (tid == 0) c.k_scale[at] = scale;
+    } else {
+      if (wave == 0) c.weight[at * CB_TOKENS + lane] = weight;
+      uint8_t* stage = smem + wave * EM_WAVE_LDS;
+      uint32_t* rows = reinterpret_cast<uint32_t*>(stage + EM_STAGE);
+      // in lines: lane = (dimension 16 n + r4, tokens 16 piece .. + 15); rows past d repeat the last one
+      const int piece = lane & 3, r4 = lane >> 2;
+      u32x4_t next[4];
+      const auto load = [&](int page_of) {
+        const int from_id = ids[page_of];
 #pragma unroll
-    for (int i = 0; i < ND; ++i) {
-      const int dim = (i * 4 + wave) * 4;
-      if (dim < d) {
-        float x[4];
-        Code<FMT>::decode(vw[i], x);
-        *reinterpret_cast<uint32_t*>(tile + lane * stride + dim) = Code<FMT>::encode(x[0] * vi, x[1] * vi, x[2] * vi, x[3] * vi);
+        for (int n = 0; n < 4; ++n) next[n] = u32x4_t{0, 0, 0, 0};
+        if (from_id >= 0 && from_id < c.blocks)
+#pragma unroll
+          for (int n = 0; n < 4; ++n)
+            next[n] = *reinterpret_cast<const u32x4_t*>(
+                c.v + (((size_t)from_id * c.hb + hh) * d + min(64 * wave + 16 * n + r4, d - 1)) * CB_TOKENS + 16 * piece);
+      };
+      const int last = __builtin_amdgcn_readlane(page, here - 1);
+      int p0 = __builtin_amdgcn_readfirstlane(page);
+      load(p0);
+      int done = 0;                                 // tokens of earlier source blocks
+      uint32_t acc = 0;                             // bytes that wait for a full word
+      for (; p0 <= last; p0 += 4) {                 // uniform; four source blocks at a time
+        // which slots of a block stay: every kept token raises the flag of the lane of its slot
+        uint64_t mine = 0;
+        int before = done;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const bool from_here = page == p0 + g;
+          const int flag = __builtin_amdgcn_ds_permute((from_here ? slot : 0) * 4, from_here ? 1 : 0);
+          // lanes without a token of this block push 0 to lane 0, which may win over a flag there
+          const uint64_t stay = (__ballot(flag) & ~1ull) | (__ballot(from_here && slot == 0) ? 1ull : 0ull);
+          if (lane >> 4 == g) { mine = stay; before = done; }
+          done += __popcll(stay);
+        }
+        // lane 16 g + i: word i of block p0 + g.  Its n kept bytes follow f that wait.
+        const int word = lane & 15;
+        const uint32_t m4 = (uint32_t)(mine >> (4 * word)) & 15u;
+        uint32_t order = 0, n8 = 0;                 // the kept bytes' numbers, 8 n
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          order |= (m4 >> e & 1) ? (uint32_t)e << n8 : 0u;
+          n8 += (m4 >> e & 1) * 8;
+        }
+        order += 0x04040404u;                       // as selectors: 4 + number, 0..3 are the waiting bytes
+        const int place = before + __popcll(mine & ((1ull << (4 * word)) - 1));
+        const uint32_t f8 = (place & 3) * 8;
+        const uint32_t fill = (0x03020100u & ((1u << f8) - 1)) | order << f8;
+        const uint32_t rest = f8 + n8 < 32 ? fill : f8 ? order >> (32 - f8) : 0u;
+        const int at_word = place >> 2;
+#pragma unroll 1
+        for (int g = 0; g < 4 && p0 + g <= last; ++g) {
+#pragma unroll
+          for (int n = 0; n < 4; ++n)               // pieces change places so that the reads below meet no bank twice
+            *reinterpret_cast<u32x4_t*>(stage + (16 * n + r4) * 64 + ((piece ^ (r4 >> 2 & 3)) << 4)) = next[n];
+          if (p0 + g < last) load(p0 + g + 1);
+          u32x4_t x[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) x[q] = *reinterpret_cast<const u32x4_t*>(stage + lane * 64 + ((q ^ (lane >> 2 & 3)) << 4));
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t s_fill = __builtin_amdgcn_readlane(fill, 16 * g + i);
+            const uint32_t s_rest = __builtin_amdgcn_readlane(rest, 16 * g + i);
+            const int s_word = __builtin_amdgcn_readlane(at_word, 16 * g + i);
+            rows[lane * EM_ROW + s_word] = __builtin_amdgcn_perm(x[i / 4][i % 4], acc, s_fill);   // word 16 is padding
+            acc = __builtin_amdgcn_perm(x[i / 4][i % 4], acc, s_rest);
+          }
+        }
       }
-    }
-    if (tid == 0) { c.k_scale[at] = ks; c.v_scale[at] = vs; }
-    if (tid < CB_TOKENS) c.weight[at * CB_TOKENS + tid] = wt;      // wave 0: lane = token
-    __syncthreads();
-    for (int e = tid; e < 4 * d; e += EM_THREADS) {
-      const int dim = e % d, t0 = e / d * 16;
-      u32x4_t o;
+      u32x4_t out[4];                               // in lines again
+      const int left = here - 16 * piece;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint32_t x = 0;
+      for (int n = 0; n < 4; ++n)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) x |= (uint32_t)tile[(t0 + 4 * q + t) * stride + dim] << (8 * t);
-        o[q] = x;
+        for (int q = 0; q < 4; ++q) {
+          const int of_word = left - 4 * q;
+          out[n][q] = rows[(16 * n + r4) * EM_ROW + 4 * piece + q] &
+                      (of_word >= 4 ? ~0u : of_word <= 0 ? 0u : (1u << (8 * of_word)) - 1);
+        }
+      const float first_scale = lane_float(old_scale, 0);
+      const bool alike = __ballot(lane < here && old_scale != first_scale) == 0;
+      float most = 0.f;
+      if (alike) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) most = largest_code<FMT>(out[n][q], most);
+        most *= first_scale;
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float s[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[e] = __shfl(old_scale, 16 * piece + 4 * q + e);
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            float y[4];
+            Code<FMT>::decode(out[n][q], y);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) most = fmaxf(most, fabsf(y[e]) * s[e]);
+          }
+        }
       }
-      *reinterpret_cast<u32x4_t*>(vo + (size_t)dim * CB_TOKENS + t0) = o;
+      const float scale = block_scale<FMT>(move_max(most, red, waves));
+      if (__ballot(lane < here && old_scale != scale)) {
+        const float ratio = move_ratio(old_scale, inverse_scale(scale));
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float s[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[e] = __shfl(ratio, 16 * piece + 4 * q + e);
+#pragma unroll
+          for (int n = 0; n < 4; ++n) out[n][q] = rescale<FMT>(out[n][q], s[0], s[1], s[2], s[3]);
+        }
+      }
+      uint8_t* vo = c.v + at * d * CB_TOKENS;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const int dim = 64 * wave + 16 * n + r4;
+        if (dim < d) __builtin_nontemporal_store(out[n], reinterpret_cast<u32x4_t*>(vo + dim * CB_TOKENS + 16 * piece));
+      }
+      if (tid == 0) c.v_scale[at] = scale;
     }
-    __syncthreads();
+    __syncthreads();                                // red is free for the next block
   }
 }
 
@@ -313,18 +461,16 @@ kvc_status launch_cache_evict(const Problem& pb, const int32_t* lengths, const i
   if (max_keep == 0) return KVC_OK;
   const int blocks = a.lpad / CB_TOKENS;
   const int64_t units = a.heads * blocks;
-  const unsigned move = (unsigned)std::min<int64_t>(units, 1 << 20);
-  const size_t lds = size_t(CB_TOKENS) * (pb.d + 4);
-#define KVC_MOVE(FMT, NU, ND) \
-  KVC_LAUNCH("evict_move", stream, evict_move<FMT, NU, ND><<<move, EM_THREADS, lds, stream>>>(a, blocks, units))
-#define KVC_MOVE_D(FMT)                       \
-  do {                                        \
-    if (pb.d <= 64) KVC_MOVE(FMT, 1, 4);      \
-    else if (pb.d <= 128) KVC_MOVE(FMT, 2, 8); \
-    else KVC_MOVE(FMT, 4, 16);                \
+  const unsigned move = (unsigned)std::min<int64_t>((units + 255) / 256 * 256, 1 << 20);
+  const int threads = (pb.d + 63) / 64 * 64;
+  const uint32_t magic = (65536 + pb.d / 16 - 1) / (pb.d / 16);   // e / (d / 16) = e * magic >> 16 for e < 1024 and d <= 256
+#define KVC_MOVE(FMT)                                                                                                     \
+  do {                                                                                                                    \
+    KVC_LAUNCH("evict_move<k>", stream, evict_move<FMT, false><<<move, threads, 0, stream>>>(a, blocks, units, magic));   \
+    KVC_LAUNCH("evict_move<v>", stream, evict_move<FMT, true><<<move, threads, threads / 64 * EM_WAVE_LDS, stream>>>(     \
+        a, blocks, units, magic));                                                                                        \
   } while (0)
-  if (format == KVC_E4M3) KVC_MOVE_D(KVC_E4M3); else KVC_MOVE_D(KVC_INT8);
-#undef KVC_MOVE_D
+  if (format == KVC_E4M3) KVC_MOVE(KVC_E4M3); else KVC_MOVE(KVC_INT8);
 #undef KVC_MOVE
   return KVC_OK;
 }

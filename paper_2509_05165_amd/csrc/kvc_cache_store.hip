@@ -114,6 +114,8 @@ __global__ __launch_bounds__(CS_THREADS) void cache_fill(PtrTable k_tab, PtrTabl
       const int e = i * CS_THREADS + tid;
       if (e < CB_TOKENS * pieces) {
         float x[8];
+        kr[i].opaque();                             // else the floats of the maximum are kept in registers until here
+        vr[i].opaque();
         kr[i].get(x);
         u32x2_t w2{Code<FMT>::encode(x[0] * ki, x[1] * ki, x[2] * ki, x[3] * ki),
                    Code<FMT>::encode(x[4] * ki, x[5] * ki, x[6] * ki, x[7] * ki)};
