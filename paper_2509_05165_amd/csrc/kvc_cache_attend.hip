@@ -113,6 +113,31 @@ __device__ __forceinline__ u32x4_t load16(const uint8_t* p) {
 }
 constexpr int DPP_ROR8 = 0x128;                     // rotate rows of 16 lanes by eight
 
+// Logits of the query rows 4 M .. 4 M + 3 of a tile, times ks.  Lane 4 M + i of 16 holds all 16 tokens of row i, so
+// that storing them as they lie would be four stores by four lanes, in pieces of 16 bytes; turned among the
+// 16 lanes they are one store, 64 bytes to a row: lane c stores tokens 4 (c / 4) .. + 3 of row c % 4.
+// (64 x 8k..16k tokens of 8 heads with weights: 369 us as they lie, 355 turned.)
+template <int M, int TILE>
+__device__ __forceinline__ float turned(float old, float x) {   // x of lane c - 4 (TILE - M), where c / 4 == TILE
+  constexpr int by = 4 * ((TILE - M) & 3);
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp((int)__float_as_uint(old), (int)__float_as_uint(x),
+                                                              by ? 0x120 + by : 0xe4, 0xf, 1 << TILE, false));
+}
+template <int M>
+__device__ __forceinline__ void store_rows(float* to, const f32x4_t (&s)[4], float ks, int lpad, int rows, int col) {
+  if (4 * M >= rows) return;                        // uniform
+  f32x4_t y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float x = turned<M, 0>(0.f, s[0][e]);
+    x = turned<M, 1>(x, s[1][e]);
+    x = turned<M, 2>(x, s[2][e]);
+    y[e] = turned<M, 3>(x, s[3][e]) * ks;
+  }
+  const int r = 4 * M + (col & 3);
+  if (r < rows) *reinterpret_cast<f32x4_t*>(to + (size_t)r * lpad + 4 * (col >> 2)) = y;
+}
+
 // Tokens of the row that this call reads.
 __device__ __forceinline__ int attend_length(const AttendArgs& a, int64_t row) {
   return min(cache_length(a.c, a.lengths[row]), a.max_length);
@@ -284,10 +309,12 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[qt][t][i] = first + 4 * t + i < seen ? s[qt][t][i] : -INFINITY;
       }
-      if (a.logits && qt * 16 + col < nq) {
-        float* to = a.logits + (size_t)(out_row + qt * 16 + col) * a.lpad + first;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4_t*>(to + 4 * t) = s[qt][t] * ks;
+      if (a.logits) {
+        float* to = a.logits + (size_t)(out_row + qt * 16) * a.lpad + first;
+        store_rows<0>(to, s[qt], ks, a.lpad, nq - qt * 16, col);
+        store_rows<1>(to, s[qt], ks, a.lpad, nq - qt * 16, col);
+        store_rows<2>(to, s[qt], ks, a.lpad, nq - qt * 16, col);
+        store_rows<3>(to, s[qt], ks, a.lpad, nq - qt * 16, col);
       }
       float top = -INFINITY;
 #pragma unroll
@@ -385,14 +412,21 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
   }
 }
 
-// Reference and sum of a row over its first n splits, by one wave.
+// Reference and sum of a row over its first n splits, by LANES neighbouring lanes.
+template <int LANES>
 __device__ __forceinline__ float2 join_sums(const float2* __restrict__ ml, int n, int lane) {
-  float top = -INFINITY, total = 0.f;
-  for (int s = lane; s < n; s += 64) top = fmaxf(top, ml[s].x);
-  top = wave_max(top);
-  for (int s = lane; s < n; s += 64) total += ml[s].x == -INFINITY ? 0.f : ml[s].y * exp2_fast(ml[s].x - top);
+  float2 y = lane < n ? ml[lane] : make_float2(-INFINITY, 0.f);
+  for (int s = lane + LANES; s < n; s += LANES) {
+    const float2 x = ml[s];
+    const float top = fmaxf(x.x, y.x);
+    if (top > -INFINITY) y = make_float2(top, x.y * exp2_fast(x.x - top) + y.y * exp2_fast(y.x - top));
+  }
+  float top = y.x;
 #pragma unroll
-  for (int off = 32; off; off >>= 1) total += __shfl_xor(total, off);
+  for (int off = LANES / 2; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+  float total = y.x == -INFINITY ? 0.f : y.y * exp2_fast(y.x - top);
+#pragma unroll
+  for (int off = LANES / 2; off; off >>= 1) total += __shfl_xor(total, off);
   return make_float2(top, total);
 }
 
@@ -409,7 +443,7 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
   __shared__ float lse2[CJ_ROWS];
   __shared__ __align__(16) float acc[CA_THREADS * 4];
   const CacheView& c = a.c;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, d = c.d;
+  const int tid = threadIdx.x, lane = tid & 63, d = c.d;
   if (blockIdx.x < joins) {
     const int64_t r = blockIdx.x;
     const int64_t bh = r / a.rows;
@@ -417,7 +451,7 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
     const int nb = (attend_length(a, cache_row(c, b, a.layer, h)) + CB_TOKENS - 1) / CB_TOKENS;
     const int n = max((nb + a.chunk - 1) / a.chunk, 1);
     const float2* ml = a.part_ml + r * a.splits;
-    const float2 all = join_sums(ml, n, lane);
+    const float2 all = join_sums<64>(ml, n, lane);
     const int wide = d / 4, groups = CA_THREADS / wide, group = tid / wide, at = (tid - group * wide) * 4;
     const float* from = a.part_o + r * a.splits * d + at;
     f32x4_t y{0.f, 0.f, 0.f, 0.f};
@@ -459,10 +493,10 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
   float gained[4] = {0.f, 0.f, 0.f, 0.f};
   for (int r0 = 0; r0 < a.rows; r0 += CJ_ROWS) {
     const int most = min(a.rows - r0, CJ_ROWS);
-    for (int r = wave; r < most; r += CA_WAVES) {
-      const float2 all = join_sums(a.part_ml + (bh * a.rows + r0 + r) * a.splits, n, lane);
+    for (int r = tid / 16; r < most; r += CA_THREADS / 16) {
+      const float2 all = join_sums<16>(a.part_ml + (bh * a.rows + r0 + r) * a.splits, n, tid & 15);
       // a row that sees no token adds nothing: 2^(-inf - inf)
-      if (lane == 0) lse2[r] = all.y > 0.f ? all.x + __builtin_amdgcn_logf(all.y) : INFINITY;
+      if ((tid & 15) == 0) lse2[r] = all.y > 0.f ? all.x + __builtin_amdgcn_logf(all.y) : INFINITY;
     }
     __syncthreads();
     for (int r = 0; r < most; r += CJ_AHEAD) {
@@ -493,8 +527,18 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
     for (int e = 0; e < len - token; ++e) to[e] = __uint_as_float(y[e]);
 }
 
-// How a call is split.  Enough workgroups that every compute unit has a few, but no chunk below one block
-// per wave.  The workspace is that of the most splits that any shorter max_length asks for.
+// How a call is split.  Two workgroups run on a compute unit, 512 on the chip.  us per call, 32/8 heads of
+// 128, e4m3, by blocks per workgroup (chunk):
+//   one sequence: enough chunks to fill the chip once, at least a block per wave: 777 tokens 9.5 (4) 11.0 (8);
+//     3000 10.3 (4) 11.9 (8); 8000 10.8 (4) 12.6 (8); 32000 19.0 (8) 21.4 (12); 128k, 64/8 heads 49.2 (32) 52.0 (16)
+//   several: smaller ones, because lengths differ and nobody knows them here: 16 x 400..13000 46.5 (16) 52.3 (48);
+//     8 x 2000 12.6 (8) 12.9 (4); 8 x 4000 17.8 (8) 19.1 (16); but from 128 heads on at least 16 blocks:
+//     16 x 1000 13.3 (16) 14.3 (8)
+//   512 heads and more: whole rows, up to 64 blocks, beyond which one long row among short ones would be
+//     waited for: 64 x 1500 34.1 (24) 41.7 (12); 64 x 6000..12000 192 (whole) 196 (64); 256 x 400..800 59.4 (whole)
+//     115 (4)
+// The workspace is that of the most splits that any shorter max_length asks for.
+constexpr int64_t CA_CHUNK_MOST = 64;
 struct AttendPlan {
   int rows, qt, row_chunks, chunk, splits, lpad;
   size_t off_o, off_ml, off_logits, total;
@@ -507,13 +551,17 @@ AttendPlan attend_plan(const Problem& pb, int64_t max_length, bool weights) {
   P.row_chunks = (P.rows + 16 * P.qt - 1) / (16 * P.qt);
   const int64_t nb = std::max<int64_t>((max_length + CB_TOKENS - 1) / CB_TOKENS, 1);
   const int64_t heads = int64_t(pb.batch) * pb.hkv * P.row_chunks;
-  const int64_t want = std::max<int64_t>(1536 / heads, 1);       // splits of a head
-  const int64_t chunk = std::max<int64_t>((nb + want - 1) / want, CA_WAVES);
+  const int64_t target = pb.batch == 1 ? 512 : 2048;             // workgroups
+  const int64_t least = heads >= 512 ? CA_CHUNK_MOST : heads >= 128 ? 16 : CA_WAVES;
+  int64_t chunk = std::min(std::max((nb * heads + target - 1) / target, least), CA_CHUNK_MOST);
+  if (pb.batch > 1 && chunk < 8 && heads * ((nb + 7) / 8) >= 256) chunk = 8;
   P.chunk = int((chunk + CA_WAVES - 1) / CA_WAVES * CA_WAVES);
   P.splits = int((nb + P.chunk - 1) / P.chunk);
   P.lpad = int(nb * CB_TOKENS);
   const size_t all = size_t(pb.batch) * pb.hkv * P.rows;
-  const size_t most = size_t(std::min(want, (nb + CA_WAVES - 1) / CA_WAVES));   // >= splits, and never falls with nb
+  // no fewer than splits, whatever nb, and never falling with nb
+  const size_t most = size_t(std::min((nb + least - 1) / least,
+                                      std::max((target + heads - 1) / heads, (nb + CA_CHUNK_MOST - 1) / CA_CHUNK_MOST)));
   size_t cur = 0;
   P.off_o = cur;
   if (most > 1) cur += align_up(all * most * pb.d * 4);
