@@ -225,46 +225,39 @@ def kvc_compress(params, q, k, v, cu_seqlens, budget, k_out, v_out, lengths, off
                               workspace_bytes, _vp(stream)), "kvc_compress")
 
 
-def _ref(struct):
-    return C.byref(struct) if struct is not None else None
-
-
+# The calls of a decoding step come once per layer and token: structs, integers and None go to ctypes as they are.
 def kvc_cache_fill(params, k, v, idx, lengths, offsets, cu_seqlens, total_budget, cache, stream=0, scores=0,
                    workspace=0, workspace_bytes=0):
-    _check(lib().kvc_cache_fill(_ref(params), _ptr_table(k), _ptr_table(v), _vp(idx), _vp(scores), _vp(lengths),
-                                _vp(offsets), _i64(cu_seqlens), total_budget, _ref(cache), _vp(workspace),
-                                workspace_bytes, _vp(stream)), "kvc_cache_fill")
+    _check(lib().kvc_cache_fill(params, _ptr_table(k), _ptr_table(v), idx, scores, lengths, offsets, _i64(cu_seqlens),
+                                total_budget, cache, workspace, workspace_bytes, stream), "kvc_cache_fill")
 
 
 def kvc_cache_append(params, layer, k_new, v_new, lengths, cache, stream=0):
-    _check(lib().kvc_cache_append(_ref(params), layer, _vp(k_new), _vp(v_new), _vp(lengths), _ref(cache),
-                                  _vp(stream)), "kvc_cache_append")
+    _check(lib().kvc_cache_append(params, layer, k_new, v_new, lengths, cache, stream), "kvc_cache_append")
 
 
 def kvc_cache_attend_workspace(params, max_length, weights=False) -> int:
     out = C.c_size_t(0)
-    _check(lib().kvc_cache_attend_workspace(_ref(params), max_length, int(weights), C.byref(out)),
-           "kvc_cache_attend_workspace")
+    _check(lib().kvc_cache_attend_workspace(params, max_length, int(weights), out), "kvc_cache_attend_workspace")
     return out.value
 
 
 def kvc_cache_attend(params, layer, q, lengths, max_length, cache, out, workspace, workspace_bytes, stream=0,
                      lse=0, weight_in=0, weight_out=0):
-    _check(lib().kvc_cache_attend(_ref(params), layer, _vp(q), _vp(lengths), max_length, _ref(cache), _vp(out),
-                                  _vp(lse), _vp(weight_in), _vp(weight_out), _vp(workspace), workspace_bytes,
-                                  _vp(stream)), "kvc_cache_attend")
+    _check(lib().kvc_cache_attend(params, layer, q, lengths, max_length, cache, out, lse, weight_in, weight_out,
+                                  workspace, workspace_bytes, stream), "kvc_cache_attend")
 
 
 def kvc_cache_evict_workspace(params, max_keep) -> int:
     out = C.c_size_t(0)
-    _check(lib().kvc_cache_evict_workspace(_ref(params), max_keep, C.byref(out)), "kvc_cache_evict_workspace")
+    _check(lib().kvc_cache_evict_workspace(params, max_keep, out), "kvc_cache_evict_workspace")
     return out.value
 
 
 def kvc_cache_evict(params, lengths, keep, max_keep, cache, table_out, lengths_out, workspace, workspace_bytes,
                     stream=0):
-    _check(lib().kvc_cache_evict(_ref(params), _vp(lengths), _vp(keep), max_keep, _ref(cache), _vp(table_out),
-                                 _vp(lengths_out), _vp(workspace), workspace_bytes, _vp(stream)), "kvc_cache_evict")
+    _check(lib().kvc_cache_evict(params, lengths, keep, max_keep, cache, table_out, lengths_out, workspace,
+                                 workspace_bytes, stream), "kvc_cache_evict")
 
 
 class _ProfileEntry(C.Structure):

@@ -374,6 +374,8 @@ __global__ __launch_bounds__(EM_THREADS) void evict_move(EvictArgs a, int blocks
           }
         }
       }
+      // bytes that the last word of all left waiting
+      if (done & 3) rows[lane * EM_ROW + (done >> 2)] = acc;
       u32x4_t out[4];                               // in lines again
       const int left = here - 16 * piece;
 #pragma unroll

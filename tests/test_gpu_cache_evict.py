@@ -96,6 +96,15 @@ def test_blocks_that_are_not_there():
     check(rng, c, [300, 200], [290, 100], lose=(1, 1))
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("n", [64, 128, 1088])
+def test_kept_tokens_up_to_the_end_of_a_block(fmt, n):
+    """The last tokens of a full block stay, and so few of the others go that they end anywhere in a word."""
+    rng = np.random.default_rng([28, n, fmt])
+    for lost in (1, 2, 3, 5, 30, 62, 63):
+        check(rng, random_cache(rng, fmt, [n], 2, 128, 1), [n], [n - lost], last=8)
+
+
 def test_scales_far_apart():
     """Rows of 2^-90 and 2^60 in one cache, rows of zeros under a large scale."""
     rng = np.random.default_rng(27)
