@@ -157,3 +157,23 @@ def test_weights_in_place_and_repeated():
     np.testing.assert_array_equal(runs[0].view(np.uint32), runs[1].view(np.uint32))
     gained = sum(float(np.nansum(runs[0][c.table[b, :n]] - c.weight[c.table[b, :n]])) for b, n in ((0, 11), (1, 1)))
     assert abs(gained - 2 * 2 * 4) < 1e-3              # two calls, two sequences, four heads
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_calls(seed):
+    rng = np.random.default_rng([33, seed])
+    layers, hkv, d = int(rng.integers(1, 3)), int(rng.integers(1, 4)), 16 * int(rng.integers(1, 17))
+    unstructured, window = bool(rng.integers(0, 2)), int(rng.choice([1, 1, 2, 5, 9]))
+    rows = int(rng.integers(1, 4)) * layers * (hkv if unstructured else 1)
+    lens = [int(x) for x in rng.integers(0, int(rng.choice([70, 300, 2000])), rows)]
+    c = random_cache(rng, int(rng.integers(0, 2)), lens, hkv, d, layers, unstructured=unstructured)
+    check(rng, c, lens, hkv * int(rng.integers(1, 9)), str(rng.choice(["bf16", "f32"])), window, int(rng.integers(0, 2)),
+          layer=int(rng.integers(0, layers)), weights=str(rng.choice(["add", "set", "none"])), q_size=float(rng.choice([0.3, 1, 4])))
+
+
+@pytest.mark.parametrize("batch,hkv,lens", [(64, 8, (1, 300)), (70, 8, (4000, 4400)), (20, 8, (1, 3000)), (9, 8, (500, 2500))])
+def test_many_heads(batch, hkv, lens):
+    """Every way in which a call is split over workgroups: whole rows, 64, 16 and 8 blocks at a time."""
+    rng = np.random.default_rng([34, batch])
+    lens = [int(x) for x in rng.integers(lens[0], lens[1], batch)]
+    check(rng, random_cache(rng, orc.E4M3, lens, hkv, 16, 1), lens, 2 * hkv)

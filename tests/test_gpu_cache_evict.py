@@ -116,3 +116,25 @@ def test_scales_far_apart():
         c.v[i, 0, :, ::2] = 0
         c.weight[i, 0, ::2] = 1.0 + j % 2
     check(rng, c, [256], [128])
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_caches(seed):
+    """Shapes, lengths, shares and weights of every kind; weights rise or fall along the row, so that what stays lies
+    in runs."""
+    rng = np.random.default_rng([29, seed])
+    layers, hkv, d = int(rng.integers(1, 4)), int(rng.integers(1, 5)), 16 * int(rng.integers(1, 17))
+    unstructured = bool(rng.integers(0, 2))
+    rows = int(rng.integers(1, 4)) * layers * (hkv if unstructured else 1)
+    most = int(rng.choice([70, 200, 700, 1500]))
+    lens = [int(x) for x in rng.integers(0, most, rows)]
+    c = random_cache(rng, int(rng.integers(0, 2)), lens, hkv, d, layers, unstructured=unstructured)
+    slope = rng.choice([-1.0, 0.0, 1.0])
+    for row, hh, *_ in c.heads():
+        for j in range(-(-lens[row] // 64)):
+            n = min(64, lens[row] - 64 * j)
+            c.weight[c.table[row, j], hh, :n] += np.float32(slope) * (64 * j + np.arange(n, dtype=np.float32)) / 64
+            if rng.random() < 0.3:
+                c.weight[c.table[row, j], hh, :n] = np.float32(rng.integers(0, 3))
+    keep = [int(round(n * s)) for n, s in zip(lens, rng.choice([0.05, 0.5, 0.9, 0.99, 1.1], rows))]
+    check(rng, c, lens, keep, first=int(rng.integers(0, 5)), last=int(rng.choice([0, 1, 16, 100])))

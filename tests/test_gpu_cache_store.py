@@ -164,3 +164,34 @@ def test_append_token_by_token_over_block_ends():
         kv.kvc_cache_append(params(c, 1, 2, "bf16"), 0, tk.data_ptr(), tv.data_ptr(), lengths.data_ptr(), device.struct, stream())
         orc.append(c, 0, k, v, [n])
     device.same(c)
+
+
+@pytest.mark.parametrize("seed", range(25))
+def test_random_fills(seed):
+    rng = np.random.default_rng([31, seed])
+    layers, hkv, d = int(rng.integers(1, 5)), int(rng.integers(1, 5)), 16 * int(rng.integers(1, 17))
+    unstructured = bool(rng.integers(0, 2))
+    lens = [int(x) for x in rng.integers(1, 300, int(rng.integers(1, 5)))]
+    per = layers * (hkv if unstructured else 1)
+    kept = [int(rng.integers(0, n + 1)) for n in lens for _ in range(per)]
+    fill_case(rng, int(rng.integers(0, 2)), str(rng.choice(["bf16", "f32"])), lens, kept, layers, hkv, d, unstructured,
+              order=int(rng.integers(0, 2)), scores=bool(rng.integers(0, 2)), offset=int(rng.integers(0, 8)))
+
+
+@pytest.mark.parametrize("seed", range(25))
+def test_random_appends(seed):
+    """Steps of any number of tokens one after the other, each of another size."""
+    rng = np.random.default_rng([32, seed])
+    hkv, d, fmt, dtype = int(rng.integers(1, 4)), 16 * int(rng.integers(1, 17)), int(rng.integers(0, 2)), str(rng.choice(["bf16", "f32"]))
+    batch = int(rng.integers(1, 5))
+    c = empty_cache(rng, fmt, [5] * batch, hkv, d, 1, width=5)
+    device, lens = Device(c), np.zeros(batch, np.int32)
+    for _ in range(6):
+        m = int(rng.integers(1, 50))
+        lens = lens + rng.integers(0, m + 1, batch).astype(np.int32)   # some rows take only the last of the m
+        k, v = (rounded(rng.standard_normal((batch, hkv, m, d)) * 2.0 ** rng.integers(-6, 7), dtype) for _ in "kv")
+        tk, tv, t_len = dev(k, dtype), dev(v, dtype), dev(lens)
+        kv.kvc_cache_append(params(c, batch, hkv, dtype, window=m), 0, tk.data_ptr(), tv.data_ptr(), t_len.data_ptr(),
+                            device.struct, stream())
+        orc.append(c, 0, k, v, lens)
+    device.same(c)
