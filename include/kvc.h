@@ -297,8 +297,8 @@ kvc_status kvc_compress(const kvc_params* params, const kvc_inputs* in,
  * between 0 and table_width*64, and a table entry outside [0, blocks) is not followed (its tokens are
  * absent: not attended to, not written, weight -infinity when evicting).  Slots behind a row's last
  * token may hold anything.  Rows may share blocks that are only read; a block that a call writes must
- * belong to one row, once.  Calls on the same blocks are ordered by their streams.  A captured
- * call reads lengths and tables when it is replayed.
+ * belong to one row, once.  Calls on the same blocks, and calls that share a workspace, must be ordered
+ * by the caller (one stream does).  A captured call reads lengths and tables when it is replayed.
  *
  * Additional limits: d a multiple of 16; k and v of the cache 16-byte aligned; table_width < 2^23.
  * Used of params: batch, layers, hq, hkv, head_dim, dtype (of rows, queries and outputs), unstructured,
@@ -351,7 +351,8 @@ kvc_status kvc_cache_append(const kvc_params* params, int32_t layer, const void*
  *   weight_out  device, laid out as the cache's weight, or NULL: for every token c of the row
  *               weight_out[c] = weight_in[c] + sum over the M queries and the G heads of its KV
  *               head of the probability of c.  weight_in NULL counts as 0; both may be the cache's weight.
- * A query that sees no token gives out = 0 and lse = -infinity.  Products on the bf16 matrix cores
+ * A query that sees no token gives out = 0 and lse = -infinity.  Values of V beyond 2^90 in size may
+ * overflow in the sums.  Products on the bf16 matrix cores
  * with fp32 accumulation: codes are bf16 numbers exactly, bf16 calls round probabilities to bf16 for
  * the product with V, fp32 calls split queries and probabilities into three bf16 terms. */
 kvc_status kvc_cache_attend(const kvc_params* params, int32_t layer, const void* q,

@@ -32,6 +32,7 @@ namespace {
 
 constexpr int CA_THREADS = 256;
 constexpr int CA_WAVES = CA_THREADS / 64;
+constexpr int CA_CHUNK_MOST = 64;                   // blocks of a workgroup, see attend_plan
 // A reference further than this below the largest logit is moved up (log2 units): sums stay below
 // 2^8 * 2^30 and rescaling is rare.
 constexpr float CA_SLACK = 8.0f;
@@ -43,11 +44,11 @@ struct AttendArgs {
   const int32_t* lengths;
   float* part_o;            // [batch * hkv * rows, splits, d]
   float2* part_ml;          // [batch * hkv * rows, splits]: reference, sum
-  float* logits;            // [batch * hkv * rows, lpad] in log2 units, or null
+  float* logits;            // [batch * hkv, lblocks, rows, 64] in log2 units, or null
   const float* weight_in;   // may be null
   float* weight_out;        // may be null
   CacheView c;
-  int layer, group, window, rows, row_chunks, splits, chunk, max_length, lpad, causal;
+  int layer, group, window, rows, row_chunks, splits, chunk, max_length, lblocks, causal;
   float scale_log2;
 };
 
@@ -124,7 +125,7 @@ __device__ __forceinline__ float turned(float old, float x) {   // x of lane c -
                                                               by ? 0x120 + by : 0xe4, 0xf, 1 << TILE, false));
 }
 template <int M>
-__device__ __forceinline__ void store_rows(float* to, const f32x4_t (&s)[4], float ks, int lpad, int rows, int col) {
+__device__ __forceinline__ void store_rows(float* to, const f32x4_t (&s)[4], float ks, int rows, int col) {
   if (4 * M >= rows) return;                        // uniform
   f32x4_t y;
 #pragma unroll
@@ -135,32 +136,13 @@ __device__ __forceinline__ void store_rows(float* to, const f32x4_t (&s)[4], flo
     y[e] = turned<M, 3>(x, s[3][e]) * ks;
   }
   const int r = 4 * M + (col & 3);
-  if (r < rows) *reinterpret_cast<f32x4_t*>(to + (size_t)r * lpad + 4 * (col >> 2)) = y;
+  if (r < rows) *reinterpret_cast<f32x4_t*>(to + r * CB_TOKENS + 4 * (col >> 2)) = y;
 }
 
 // Tokens of the row that this call reads.
 __device__ __forceinline__ int attend_length(const AttendArgs& a, int64_t row) {
   return min(cache_length(a.c, a.lengths[row]), a.max_length);
 }
-
-// The blocks of a wave: their ids and scales, 64 at a time in the lanes of three registers.
-struct BlockList {
-  int ids;
-  float ks, vs;
-  // p: block of lane 0; lane i holds block p + CA_WAVES * i
-  __device__ __forceinline__ void load(const AttendArgs& a, int64_t row, int hh, int p, int hi, int lane) {
-    const int at = p + CA_WAVES * lane;
-    ids = at < hi ? a.c.table[row * a.c.width + at] : -1;
-    if (ids >= a.c.blocks) ids = -1;
-    const size_t s = (size_t)max(ids, 0) * a.c.hb + hh;
-    ks = a.c.k_scale[s];
-    vs = a.c.v_scale[s];
-  }
-  __device__ __forceinline__ int id(int i) const { return __builtin_amdgcn_readlane(ids, i & 63); }
-  static __device__ __forceinline__ float lane_of(float x, int i) {
-    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i & 63));
-  }
-};
 
 // NJ: groups of 64 dimensions, d = 64 * NJ where EXACT; QT: tiles of 16 query rows per workgroup.
 // grid: (splits * row_chunks * hkv, 1, batch), the head fastest: with 8 heads all row chunks of a head
@@ -182,13 +164,19 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
   const int split = x / a.row_chunks, rc = x - split * a.row_chunks;
   const int64_t row = cache_row(c, b, a.layer, h);
   const int hh = cache_head(c, h);
+  const int lo = split * a.chunk, first_block = lo + __builtin_amdgcn_readfirstlane(wave);
+  // The blocks of this wave, one per lane (asked for before the length is known): ids and scales.
+  static_assert(CA_CHUNK_MOST / CA_WAVES <= 64, "a lane for every block of a wave");
+  const int my_block = first_block + CA_WAVES * lane;
+  int my_id = c.table[row * c.width + min(my_block, c.width - 1)];
   const int len = attend_length(a, row);
   const int nb = (len + CB_TOKENS - 1) / CB_TOKENS;
-  const int lo = split * a.chunk, hi = min(lo + a.chunk, nb);
+  const int hi = min(lo + a.chunk, nb);
   if (split > 0 && lo >= nb) return;                // attend_join knows that this split is empty
-  const int first_block = lo + __builtin_amdgcn_readfirstlane(wave);
-  BlockList list;
-  list.load(a, row, hh, first_block, hi, lane);
+  if (my_block >= hi || my_id >= c.blocks) my_id = -1;
+  const size_t my_scale = (size_t)max(my_id, 0) * c.hb + hh;
+  const float my_ks = c.k_scale[my_scale], my_vs = c.v_scale[my_scale];
+  const auto lane_of = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
   const int r0 = rc * 16 * QT, nq = min(a.rows - r0, 16 * QT);
   const int64_t out_row = ((int64_t)b * c.hkv + h) * a.rows + r0;
 
@@ -228,7 +216,7 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
                             : __builtin_amdgcn_update_dpp(even, odd, DPP_ROR8, 0xf, 0xc, false));
   };
   if (first_block < hi) {
-    const int id = list.id(0);
+    const int id = __builtin_amdgcn_readfirstlane(my_id);
     load_k(id);
     load_v(id);
   }
@@ -266,11 +254,11 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
 
   int it = 0;
   for (int p = first_block; p < hi; p += CA_WAVES, ++it) {
-    const int id = list.id(it);
-    const float ks = BlockList::lane_of(list.ks, it) * a.scale_log2, vs = BlockList::lane_of(list.vs, it);
+    const int id = __builtin_amdgcn_readlane(my_id, it);
+    // (a scale that is too small for a normal number gives logits of 0, and -infinity stays what it is)
+    const float ks = fmaxf(lane_of(my_ks, it) * a.scale_log2, 1.17549435e-38f), vs = lane_of(my_vs, it);
     const bool more = p + CA_WAVES < hi;
-    if (more && ((it + 1) & 63) == 0) list.load(a, row, hh, p + CA_WAVES, hi, lane);
-    const int next = list.id(it + 1);
+    const int next = __builtin_amdgcn_readlane(my_id, (it + 1) & 63);
 
     // ---- logits ----
     f32x4_t s[QT][4];
@@ -310,11 +298,11 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
           for (int i = 0; i < 4; ++i) s[qt][t][i] = first + 4 * t + i < seen ? s[qt][t][i] : -INFINITY;
       }
       if (a.logits) {
-        float* to = a.logits + (size_t)(out_row + qt * 16) * a.lpad + first;
-        store_rows<0>(to, s[qt], ks, a.lpad, nq - qt * 16, col);
-        store_rows<1>(to, s[qt], ks, a.lpad, nq - qt * 16, col);
-        store_rows<2>(to, s[qt], ks, a.lpad, nq - qt * 16, col);
-        store_rows<3>(to, s[qt], ks, a.lpad, nq - qt * 16, col);
+        float* to = a.logits + ((((size_t)b * c.hkv + h) * a.lblocks + p) * a.rows + r0 + qt * 16) * CB_TOKENS + 16 * g;
+        store_rows<0>(to, s[qt], ks, nq - qt * 16, col);
+        store_rows<1>(to, s[qt], ks, nq - qt * 16, col);
+        store_rows<2>(to, s[qt], ks, nq - qt * 16, col);
+        store_rows<3>(to, s[qt], ks, nq - qt * 16, col);
       }
       float top = -INFINITY;
 #pragma unroll
@@ -483,10 +471,11 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
   const int n = max(((len + CB_TOKENS - 1) / CB_TOKENS + a.chunk - 1) / a.chunk, 1);
   const int id = token < len ? c.table[row * c.width + token / CB_TOKENS] : -1;
   const bool on = id >= 0 && id < c.blocks;
-  const float* from = a.logits + (size_t)(bh * a.rows) * a.lpad + (on ? token : 0);
+  const int known = on ? token : 0;
+  const float* from = a.logits + ((size_t)bh * a.lblocks + known / CB_TOKENS) * a.rows * CB_TOKENS + known % CB_TOKENS;
   f32x4_t s[CJ_AHEAD];
 #pragma unroll
-  for (int i = 0; i < CJ_AHEAD; ++i) s[i] = *reinterpret_cast<const f32x4_t*>(from + (size_t)min(i, a.rows - 1) * a.lpad);
+  for (int i = 0; i < CJ_AHEAD; ++i) s[i] = *reinterpret_cast<const f32x4_t*>(from + min(i, a.rows - 1) * CB_TOKENS);
   const size_t at = ((size_t)(on ? id : 0) * c.hb + cache_head(c, h)) * CB_TOKENS + token % CB_TOKENS;
   u32x4_word w_in{0, 0, 0, 0};
   if (on && a.weight_in) w_in = *reinterpret_cast<const u32x4_word*>(a.weight_in + at);
@@ -506,7 +495,7 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
       if (r0 + r + CJ_AHEAD < a.rows)
 #pragma unroll
         for (int i = 0; i < CJ_AHEAD; ++i)
-          s[i] = *reinterpret_cast<const f32x4_t*>(from + (size_t)min(r0 + r + CJ_AHEAD + i, a.rows - 1) * a.lpad);
+          s[i] = *reinterpret_cast<const f32x4_t*>(from + (size_t)min(r0 + r + CJ_AHEAD + i, a.rows - 1) * CB_TOKENS);
 #pragma unroll
       for (int i = 0; i < CJ_AHEAD; ++i)
         if (r + i < most) {
@@ -538,9 +527,8 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
 //     waited for: 64 x 1500 34.1 (24) 41.7 (12); 64 x 6000..12000 192 (whole) 196 (64); 256 x 400..800 59.4 (whole)
 //     115 (4)
 // The workspace is that of the most splits that any shorter max_length asks for.
-constexpr int64_t CA_CHUNK_MOST = 64;
 struct AttendPlan {
-  int rows, qt, row_chunks, chunk, splits, lpad;
+  int rows, qt, row_chunks, chunk, splits, lblocks;
   size_t off_o, off_ml, off_logits, total;
 };
 
@@ -552,12 +540,12 @@ AttendPlan attend_plan(const Problem& pb, int64_t max_length, bool weights) {
   const int64_t nb = std::max<int64_t>((max_length + CB_TOKENS - 1) / CB_TOKENS, 1);
   const int64_t heads = int64_t(pb.batch) * pb.hkv * P.row_chunks;
   const int64_t target = pb.batch == 1 ? 512 : 2048;             // workgroups
-  const int64_t least = heads >= 512 ? CA_CHUNK_MOST : heads >= 128 ? 16 : CA_WAVES;
-  int64_t chunk = std::min(std::max((nb * heads + target - 1) / target, least), CA_CHUNK_MOST);
+  const int64_t least = heads >= 512 ? int64_t(CA_CHUNK_MOST) : heads >= 128 ? 16 : CA_WAVES;
+  int64_t chunk = std::min(std::max((nb * heads + target - 1) / target, least), int64_t(CA_CHUNK_MOST));
   if (pb.batch > 1 && chunk < 8 && heads * ((nb + 7) / 8) >= 256) chunk = 8;
   P.chunk = int((chunk + CA_WAVES - 1) / CA_WAVES * CA_WAVES);
   P.splits = int((nb + P.chunk - 1) / P.chunk);
-  P.lpad = int(nb * CB_TOKENS);
+  P.lblocks = int(nb);
   const size_t all = size_t(pb.batch) * pb.hkv * P.rows;
   // no fewer than splits, whatever nb, and never falling with nb
   const size_t most = size_t(std::min((nb + least - 1) / least,
@@ -568,7 +556,7 @@ AttendPlan attend_plan(const Problem& pb, int64_t max_length, bool weights) {
   P.off_ml = cur;
   if (most > 1 || weights) cur += align_up(all * most * 8);
   P.off_logits = cur;
-  if (weights) cur += align_up(all * size_t(P.lpad) * 4);
+  if (weights) cur += align_up(all * size_t(P.lblocks) * CB_TOKENS * 4);
   P.total = cur;
   return P;
 }
@@ -628,7 +616,7 @@ kvc_status launch_cache_attend(const Problem& pb, int layer, const void* q, cons
   a.weight_in = weight_in; a.weight_out = weight_out;
   a.c = c;
   a.layer = layer; a.group = pb.group; a.window = pb.window; a.rows = P.rows; a.row_chunks = P.row_chunks;
-  a.splits = P.splits; a.chunk = P.chunk; a.max_length = int(max_length); a.lpad = P.lpad; a.causal = pb.causal_tail;
+  a.splits = P.splits; a.chunk = P.chunk; a.max_length = int(max_length); a.lblocks = P.lblocks; a.causal = pb.causal_tail;
   a.scale_log2 = pb.scale * 1.4426950408889634f;
   const unsigned grid = unsigned(P.splits) * P.row_chunks * pb.hkv;
   const bool half = pb.dtype == KVC_BF16;

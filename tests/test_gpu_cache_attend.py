@@ -134,6 +134,16 @@ def test_extreme_logits(fmt):
         check(rng, c, [500], 4, "bf16", q_size=size, scale=scale)
 
 
+def test_scales_at_their_ends():
+    """Blocks of the least scale, values of 2^88, a softmax scale that no product with it survives."""
+    rng = np.random.default_rng(35)
+    for e, scale in ((-100, 0.0), (80, 0.0), (-100, 1e-30)):
+        c = random_cache(rng, orc.INT8, [150, 0], 2, 32, 1)
+        c.v_scale[c.table[0, 1]] = np.float32(2.0 ** e)
+        c.k_scale[c.table[0, 0]] = np.float32(2.0 ** -100)
+        check(rng, c, [150, 0], 4, "f32", window=2, causal=1, scale=scale)
+
+
 def test_pointers_off_sixteen_bytes():
     rng = np.random.default_rng(18)
     for dtype in ("bf16", "f32"):
