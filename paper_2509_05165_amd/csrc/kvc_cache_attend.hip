@@ -45,6 +45,7 @@ struct AttendArgs {
   float* part_o;            // [batch * hkv * rows, splits, d]
   float2* part_ml;          // [batch * hkv * rows, splits]: reference, sum
   float* logits;            // [batch * hkv, lblocks, rows, 64] in log2 units, or null
+  int kept;                 // or where in LDS a workgroup that takes whole rows keeps them (0: not)
   const float* weight_in;   // may be null
   float* weight_out;        // may be null
   CacheView c;
@@ -155,8 +156,8 @@ template <int FMT, typename T, int NJ, bool EXACT, int QT, bool STREAM>
 __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void attend_split(AttendArgs a) {
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
   constexpr int NT = 4 * NJ;                        // tiles of 16 dimensions
-  extern __shared__ __align__(16) float lds[];      // [waves][nq][d], nq = query rows of this workgroup
-  __shared__ float sm[CA_WAVES][16 * QT], sl[CA_WAVES][16 * QT];
+  extern __shared__ __align__(16) float lds[];      // [waves][nq][d], nq = query rows of this workgroup; at kept [chunk][nq][64]
+  __shared__ float sm[CA_WAVES][16 * QT], sl[CA_WAVES][16 * QT], lse2[16 * QT];
   const CacheView& c = a.c;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int d = EXACT ? 64 * NJ : c.d, b = blockIdx.z;
@@ -297,7 +298,13 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[qt][t][i] = first + 4 * t + i < seen ? s[qt][t][i] : -INFINITY;
       }
-      if (a.logits) {
+      if (a.kept) {
+        float* to = lds + a.kept + (size_t)((p - lo) * nq + qt * 16) * CB_TOKENS + 16 * g;
+        store_rows<0>(to, s[qt], ks, nq - qt * 16, col);
+        store_rows<1>(to, s[qt], ks, nq - qt * 16, col);
+        store_rows<2>(to, s[qt], ks, nq - qt * 16, col);
+        store_rows<3>(to, s[qt], ks, nq - qt * 16, col);
+      } else if (a.logits) {
         float* to = a.logits + ((((size_t)b * c.hkv + h) * a.lblocks + p) * a.rows + r0 + qt * 16) * CB_TOKENS + 16 * g;
         store_rows<0>(to, s[qt], ks, nq - qt * 16, col);
         store_rows<1>(to, s[qt], ks, nq - qt * 16, col);
@@ -396,7 +403,20 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
     } else {
       *reinterpret_cast<f32x4_t*>(a.part_o + ((out_row + r) * a.splits + split) * d + at) = y;
     }
+    if (at == 0) lse2[r] = total > 0.f ? top + __builtin_amdgcn_logf(total) : INFINITY;
     if (at == 0 && a.part_ml) a.part_ml[(out_row + r) * a.splits + split] = make_float2(top, total);
+  }
+  if (a.kept) {                                     // the logits of the whole row are here: its weights too
+    __syncthreads();
+    for (int token = tid; token < len; token += CA_THREADS) {
+      const int id = c.table[row * c.width + token / CB_TOKENS];
+      if (id < 0 || id >= c.blocks) continue;
+      const size_t at = ((size_t)id * c.hb + hh) * CB_TOKENS + token % CB_TOKENS;
+      const float* logit = lds + a.kept + (token / CB_TOKENS) * nq * CB_TOKENS + token % CB_TOKENS;
+      float gained = 0.f;                           // small beside what is there: added to it once
+      for (int r = 0; r < nq; ++r) gained += exp2_fast(logit[r * CB_TOKENS] - lse2[r]);   // no token seen: 2^(-inf - inf)
+      a.weight_out[at] = a.weight_in ? a.weight_in[at] + gained : gained;
+    }
   }
 }
 
@@ -526,9 +546,15 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
 //   512 heads and more: whole rows, up to 64 blocks, beyond which one long row among short ones would be
 //     waited for: 64 x 1500 34.1 (24) 41.7 (12); 64 x 6000..12000 192 (whole) 196 (64); 256 x 400..800 59.4 (whole)
 //     115 (4)
-// The workspace is that of the most splits that any shorter max_length asks for.
+// Where whole rows of a head are one workgroup's work and their logits fit into LDS beside what joins the waves,
+// weights are gathered there and then; else the logits go through the workspace to attend_join.  With
+// weights, LDS / memory: 64 x 4000 tokens of 32/8 heads (63 KB of logits) 91 / 115 us, of 64/8 heads (126 KB, one
+// workgroup to a compute unit) 116 / 131; 256 x 400..800 68 / 80.
+// The workspace is that of the most splits that any shorter max_length asks for, with its logits.
+constexpr int64_t CA_LDS = 152 << 10;               // of 160 KB
 struct AttendPlan {
   int rows, qt, row_chunks, chunk, splits, lblocks;
+  bool kept;                                        // logits stay in LDS
   size_t off_o, off_ml, off_logits, total;
 };
 
@@ -546,6 +572,7 @@ AttendPlan attend_plan(const Problem& pb, int64_t max_length, bool weights) {
   P.chunk = int((chunk + CA_WAVES - 1) / CA_WAVES * CA_WAVES);
   P.splits = int((nb + P.chunk - 1) / P.chunk);
   P.lblocks = int(nb);
+  P.kept = weights && P.splits == 1 && P.row_chunks == 1 && (nb * CB_TOKENS + CA_WAVES * pb.d) * P.rows * 4 <= CA_LDS;
   const size_t all = size_t(pb.batch) * pb.hkv * P.rows;
   // no fewer than splits, whatever nb, and never falling with nb
   const size_t most = size_t(std::min((nb + least - 1) / least,
@@ -564,7 +591,8 @@ AttendPlan attend_plan(const Problem& pb, int64_t max_length, bool weights) {
 template <int FMT, typename T>
 kvc_status attend_form(const Problem& pb, const AttendPlan& P, const AttendArgs& a, unsigned grid, hipStream_t stream) {
   const dim3 g(grid, 1, pb.batch);
-  const size_t lds = size_t(CA_WAVES) * std::min(P.rows, 16 * P.qt) * pb.d * 4;
+  const size_t lds = size_t(CA_WAVES) * std::min(P.rows, 16 * P.qt) * pb.d * 4 +
+                     (P.kept ? size_t(P.lblocks) * P.rows * CB_TOKENS * 4 : 0);
 #define KVC_ATTEND(NJ, QT, STREAM)                                                                                        \
   do {                                                                                                                    \
     if (pb.d == 64 * NJ)                                                                                                  \
@@ -612,7 +640,8 @@ kvc_status launch_cache_attend(const Problem& pb, int layer, const void* q, cons
   a.q = q; a.out = out; a.lse = lse; a.lengths = lengths;
   a.part_o = reinterpret_cast<float*>(base + P.off_o);
   a.part_ml = P.splits > 1 || weights ? reinterpret_cast<float2*>(base + P.off_ml) : nullptr;
-  a.logits = weights ? reinterpret_cast<float*>(base + P.off_logits) : nullptr;
+  a.kept = P.kept ? CA_WAVES * P.rows * pb.d : 0;
+  a.logits = weights && !P.kept ? reinterpret_cast<float*>(base + P.off_logits) : nullptr;
   a.weight_in = weight_in; a.weight_out = weight_out;
   a.c = c;
   a.layer = layer; a.group = pb.group; a.window = pb.window; a.rows = P.rows; a.row_chunks = P.row_chunks;
@@ -629,7 +658,7 @@ kvc_status launch_cache_attend(const Problem& pb, int layer, const void* q, cons
   const int64_t heads = int64_t(pb.batch) * pb.hkv;
   const int64_t joins = P.splits > 1 ? heads * P.rows : 0;
   const int chunks = int((max_length + CJ_TOKENS - 1) / CJ_TOKENS);
-  const int64_t total = joins + (weights ? heads * chunks : 0);
+  const int64_t total = joins + (weights && !P.kept ? heads * chunks : 0);
   if (total == 0) return KVC_OK;
 #define KVC_JOIN(T) \
   KVC_LAUNCH("attend_join", stream, attend_join<T><<<(unsigned)total, CA_THREADS, 0, stream>>>(a, joins, std::max(chunks, 1)))

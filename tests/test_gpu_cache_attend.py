@@ -187,3 +187,13 @@ def test_many_heads(batch, hkv, lens):
     rng = np.random.default_rng([34, batch])
     lens = [int(x) for x in rng.integers(lens[0], lens[1], batch)]
     check(rng, random_cache(rng, orc.E4M3, lens, hkv, 16, 1), lens, 2 * hkv)
+
+
+@pytest.mark.parametrize("group,window,weights", [(1, 1, "add"), (4, 1, "set"), (8, 1, "add"), (9, 1, "add"), (3, 3, "set"), (20, 1, "add")])
+def test_weights_of_whole_rows(group, window, weights):
+    """Heads enough for whole rows: logits in LDS (up to 126 KB of them and no longer), holes in the table."""
+    rng = np.random.default_rng([36, group, window])
+    lens = [int(x) for x in rng.integers(0, 1500, 63)] + [4096 if group <= 9 else 1500]
+    c = random_cache(rng, orc.INT8, lens, 8, 16, 1)
+    c.table[5, 1] = -1
+    check(rng, c, lens, 8 * group, window=window, causal=int(window > 1), weights=weights)
