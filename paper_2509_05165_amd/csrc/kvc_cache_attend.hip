@@ -167,7 +167,7 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
   const int hh = cache_head(c, h);
   const int lo = split * a.chunk, first_block = lo + __builtin_amdgcn_readfirstlane(wave);
   // The blocks of this wave, one per lane (asked for before the length is known): ids and scales.
-  static_assert(CA_CHUNK_MOST / CA_WAVES <= 64, "a lane for every block of a wave");
+  // (a chunk has at most 64 * CA_WAVES blocks)
   const int my_block = first_block + CA_WAVES * lane;
   int my_id = c.table[row * c.width + min(my_block, c.width - 1)];
   const int len = attend_length(a, row);
@@ -546,10 +546,12 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
 //   512 heads and more: whole rows, up to 64 blocks, beyond which one long row among short ones would be
 //     waited for: 64 x 1500 34.1 (24) 41.7 (12); 64 x 6000..12000 192 (whole) 196 (64); 256 x 400..800 59.4 (whole)
 //     115 (4)
-// Where whole rows of a head are one workgroup's work and their logits fit into LDS beside what joins the waves,
-// weights are gathered there and then; else the logits go through the workspace to attend_join.  With
-// weights, LDS / memory: 64 x 4000 tokens of 32/8 heads (63 KB of logits) 91 / 115 us, of 64/8 heads (126 KB, one
-// workgroup to a compute unit) 116 / 131; 256 x 400..800 68 / 80.
+// With weights, where whole rows of a head are one workgroup's work and their logits fit into LDS beside what joins
+// the waves, weights are gathered there and then; else the logits go through the workspace to attend_join.
+// LDS / memory: 64 x 4000 tokens of 32/8 heads (63 KB of logits) 91 / 115 us, of 64/8 heads (126 KB, one
+// workgroup to a compute unit) 116 / 131; 256 x 400..800 68 / 80.  So from 256 heads on rows stay whole where that
+// makes them fit (whole / split): 64 x 8000 218 / 231, 32 x 4000 59 / 65, 32 x 1500 26 / 33; with 128 heads it
+// does not pay: 16 x 4000 46 / 36.
 // The workspace is that of the most splits that any shorter max_length asks for, with its logits.
 constexpr int64_t CA_LDS = 152 << 10;               // of 160 KB
 struct AttendPlan {
@@ -569,10 +571,13 @@ AttendPlan attend_plan(const Problem& pb, int64_t max_length, bool weights) {
   const int64_t least = heads >= 512 ? int64_t(CA_CHUNK_MOST) : heads >= 128 ? 16 : CA_WAVES;
   int64_t chunk = std::min(std::max((nb * heads + target - 1) / target, least), int64_t(CA_CHUNK_MOST));
   if (pb.batch > 1 && chunk < 8 && heads * ((nb + 7) / 8) >= 256) chunk = 8;
+  const bool fits = weights && P.row_chunks == 1 && nb <= 64 * CA_WAVES &&
+                    (nb * CB_TOKENS + CA_WAVES * pb.d) * P.rows * 4 <= CA_LDS;
+  if (fits && heads >= 256) chunk = std::max(chunk, nb);
   P.chunk = int((chunk + CA_WAVES - 1) / CA_WAVES * CA_WAVES);
   P.splits = int((nb + P.chunk - 1) / P.chunk);
   P.lblocks = int(nb);
-  P.kept = weights && P.splits == 1 && P.row_chunks == 1 && (nb * CB_TOKENS + CA_WAVES * pb.d) * P.rows * 4 <= CA_LDS;
+  P.kept = fits && P.splits == 1;
   const size_t all = size_t(pb.batch) * pb.hkv * P.rows;
   // no fewer than splits, whatever nb, and never falling with nb
   const size_t most = size_t(std::min((nb + least - 1) / least,

@@ -181,6 +181,14 @@ def test_random_calls(seed):
           layer=int(rng.integers(0, layers)), weights=str(rng.choice(["add", "set", "none"])), q_size=float(rng.choice([0.3, 1, 4])))
 
 
+def test_weights_of_long_whole_rows():
+    """More than 64 blocks to a workgroup: one query row to a head, rows up to the most that LDS holds."""
+    rng = np.random.default_rng(37)
+    lens = [int(x) for x in rng.integers(0, 300, 32)]
+    lens[3], lens[30] = 16384, 9001
+    check(rng, random_cache(rng, orc.E4M3, lens, 8, 16, 1), lens, 8)
+
+
 @pytest.mark.parametrize("batch,hkv,lens", [(64, 8, (1, 300)), (70, 8, (4000, 4400)), (20, 8, (1, 3000)), (9, 8, (500, 2500))])
 def test_many_heads(batch, hkv, lens):
     """Every way in which a call is split over workgroups: whole rows, 64, 16 and 8 blocks at a time."""
