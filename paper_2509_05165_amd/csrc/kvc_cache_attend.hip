@@ -6,9 +6,10 @@
 //   out[r,:] = sum_c p[r,c] vs(block) vc[c,:] / sum_c p[r,c]
 // Codes of both formats are bf16 numbers exactly, so both products run on the bf16 matrix cores with
 // fp32 accumulation; the scales are applied to the fp32 logits and to the fp32 probabilities
-// (exactly, they are powers of two).  bf16 calls round the probabilities to bf16 for the second product
-// (half a step, 2^-8 relative, which is what the output's own rounding costs); float32 calls split
-// queries and probabilities into three bf16 terms each, 24 bits, and lose nothing.
+// (exactly, they are powers of two).  For the second product bf16 calls round the probabilities to two bf16
+// terms, 16 bits, or, with more than 16 query rows to a KV head, to one (half a step, 2^-8 relative, as much as the
+// output's own rounding); float32 calls split queries and probabilities into three terms each, 24
+// bits, and lose nothing.
 //
 // Layout: v_mfma_f32_16x16x32_bf16 with tokens on the rows and queries on the columns of the first
 // product.  A wave takes a block of 64 tokens as four tiles; tile t holds the tokens 16*g + 4*t + i
@@ -154,7 +155,11 @@ __device__ __forceinline__ int attend_length(const AttendArgs& a, int64_t row) {
 // as this block's output is.
 template <int FMT, typename T, int NJ, bool EXACT, int QT, bool STREAM>
 __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void attend_split(AttendArgs a) {
-  constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;
+  // Terms of the queries and of the probabilities.  bf16 calls: queries are one term; a second one for the
+  // probabilities (16 bits) is free where the codes bound the kernel (64 x 16k tokens, 32/8 heads 335.9 us with one, 338.7
+  // with two; output error against float64 2.4e-3 -> 1.7e-3, its own rounding) and costs where 32 rows share them
+  // (M = 8: 433 / 484).
+  constexpr int TERMS = sizeof(T) == 2 ? 1 : 3, PTERMS = sizeof(T) == 2 ? (QT == 1 ? 2 : 1) : 3;
   constexpr int NT = 4 * NJ;                        // tiles of 16 dimensions
   extern __shared__ __align__(16) float lds[];      // [waves][nq][d], nq = query rows of this workgroup; at kept [chunk][nq][64]
   __shared__ float sm[CA_WAVES][16 * QT], sl[CA_WAVES][16 * QT], lse2[16 * QT];
@@ -288,7 +293,7 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
     const bool tail = (p + 1) * CB_TOKENS > here - (a.causal ? a.window - 1 : 0);   // wave-uniform
     const float shift = __builtin_amdgcn_logf(vs);  // whole: vs is a power of two
     const float inv_vs = inverse_scale(vs);
-    bf16x8_t pf[QT][2][TERMS];
+    bf16x8_t pf[QT][2][PTERMS];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       if (tail) {
@@ -338,7 +343,7 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
         }
       sum[qt] = fmaf(part, inv_vs, sum[qt]);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) split_terms<TERMS>(pr[u], pf[qt][u]);
+      for (int u = 0; u < 2; ++u) split_terms<PTERMS>(pr[u], pf[qt][u]);
     }
     // ---- values ----
     if ((p + 1) * CB_TOKENS > here) {               // slots behind the last token hold anything: no code 0 times NaN
@@ -358,7 +363,7 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
-          for (int m = TERMS - 1; m >= 0; --m)
+          for (int m = PTERMS - 1; m >= 0; --m)
             o[qt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt][u][m], o[qt][n], 0, 0, 0);
         if (n % 4 == 3) __builtin_amdgcn_sched_barrier(0);
       }
