@@ -181,7 +181,8 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
   if (split > 0 && lo >= nb) return;                // attend_join knows that this split is empty
   if (my_block >= hi || my_id >= c.blocks) my_id = -1;
   const size_t my_scale = (size_t)max(my_id, 0) * c.hb + hh;
-  const float my_ks = c.k_scale[my_scale], my_vs = c.v_scale[my_scale];
+  // (an entry that names no block: block 0 is loaded in its place, whatever it holds, and masked; 1 as its scales)
+  const float my_ks = my_id < 0 ? 1.0f : c.k_scale[my_scale], my_vs = my_id < 0 ? 1.0f : c.v_scale[my_scale];
   const auto lane_of = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
   const int r0 = rc * 16 * QT, nq = min(a.rows - r0, 16 * QT);
   const int64_t out_row = ((int64_t)b * c.hkv + h) * a.rows + r0;

@@ -111,6 +111,24 @@ def test_bounds_and_blocks_that_are_not_there():
         check(rng, c, lens, 4, max_length=most)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_first_block_of_the_pool_is_nobodys(dtype):
+    """Block 0, which stands in for entries that name no block, holds NaN codes and NaN scales."""
+    rng = np.random.default_rng(38)
+    c = random_cache(rng, orc.E4M3, [300, 64], 2, 64, 1)
+    spare = int(np.setdiff1d(np.arange(len(c.k)), np.concatenate([c.table[0, :5], c.table[1, :1]]))[-1])
+    if (c.table == 0).any() and spare:
+        for name in ("k", "v", "k_scale", "v_scale", "weight"):
+            getattr(c, name)[spare] = getattr(c, name)[0]
+        c.table[c.table == 0] = spare
+    c.k[0] = c.v[0] = 0x7F
+    c.k_scale[0] = c.v_scale[0] = np.nan
+    c.table[0, 1] = -1
+    c.table[1, 0] = 1 << 30                           # nothing of this row is there
+    for weights in ("add", "none"):
+        check(rng, c, [300, 64], 4, dtype, weights=weights)
+
+
 def test_layers_and_heads_with_rows_of_their_own():
     rng = np.random.default_rng(16)
     lens = list(rng.integers(0, 200, 2 * 3 * 4))
