@@ -46,7 +46,7 @@ struct AttendArgs {
   float* part_o;            // [batch * hkv * rows, splits, d]
   float2* part_ml;          // [batch * hkv * rows, splits]: reference, sum
   float* logits;            // [batch * hkv, lblocks, rows, 64] in log2 units, or null
-  int kept;                 // or where in LDS a workgroup that takes whole rows keeps them (0: not)
+  int kept, kept_blocks;    // where in LDS a workgroup that takes whole rows keeps those of its first blocks (0: nowhere)
   const float* weight_in;   // may be null
   float* weight_out;        // may be null
   CacheView c;
@@ -146,6 +146,25 @@ __device__ __forceinline__ int attend_length(const AttendArgs& a, int64_t row) {
   return min(cache_length(a.c, a.lengths[row]), a.max_length);
 }
 
+// weight_out = weight_in + gained for four tokens of a block; those of a block that is not there have no weight.
+__device__ __forceinline__ void add_weights(const AttendArgs& a, int64_t row, int hh, int token, int len, f32x4_t gained) {
+  const CacheView& c = a.c;
+  const int id = c.table[row * c.width + token / CB_TOKENS];
+  if (id < 0 || id >= c.blocks) return;
+  const size_t at = ((size_t)id * c.hb + hh) * CB_TOKENS + token % CB_TOKENS;
+  if (token + 4 <= len) {
+    u32x4_word w{0, 0, 0, 0}, y;
+    if (a.weight_in) w = *reinterpret_cast<const u32x4_word*>(a.weight_in + at);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = __float_as_uint(__uint_as_float(w[e]) + gained[e]);
+    *reinterpret_cast<u32x4_word*>(a.weight_out + at) = y;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (token + e < len) a.weight_out[at + e] = (a.weight_in ? a.weight_in[at + e] : 0.f) + gained[e];
+  }
+}
+
 // NJ: groups of 64 dimensions, d = 64 * NJ where EXACT; QT: tiles of 16 query rows per workgroup.
 // grid: (splits * row_chunks * hkv, 1, batch), the head fastest: with 8 heads all row chunks of a head
 // run on the same chiplet and share its L2.
@@ -161,7 +180,7 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
   // (M = 8: 433 / 484).
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 3, PTERMS = sizeof(T) == 2 ? (QT == 1 ? 2 : 1) : 3;
   constexpr int NT = 4 * NJ;                        // tiles of 16 dimensions
-  extern __shared__ __align__(16) float lds[];      // [waves][nq][d], nq = query rows of this workgroup; at kept [chunk][nq][64]
+  extern __shared__ __align__(16) float lds[];      // [waves][nq][d], nq = query rows of this workgroup; at kept [kept_blocks][nq][64]
   __shared__ float sm[CA_WAVES][16 * QT], sl[CA_WAVES][16 * QT], lse2[16 * QT];
   const CacheView& c = a.c;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
@@ -304,7 +323,7 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[qt][t][i] = first + 4 * t + i < seen ? s[qt][t][i] : -INFINITY;
       }
-      if (a.kept) {
+      if (p < a.kept_blocks) {
         float* to = lds + a.kept + (size_t)((p - lo) * nq + qt * 16) * CB_TOKENS + 16 * g;
         store_rows<0>(to, s[qt], ks, nq - qt * 16, col);
         store_rows<1>(to, s[qt], ks, nq - qt * 16, col);
@@ -412,16 +431,27 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
     if (at == 0) lse2[r] = total > 0.f ? top + __builtin_amdgcn_logf(total) : INFINITY;
     if (at == 0 && a.part_ml) a.part_ml[(out_row + r) * a.splits + split] = make_float2(top, total);
   }
-  if (a.kept) {                                     // the logits of the whole row are here: its weights too
+  if (a.kept) {                                     // the logits of the whole row are this workgroup's: its weights too
     __syncthreads();
-    for (int token = tid; token < len; token += CA_THREADS) {
-      const int id = c.table[row * c.width + token / CB_TOKENS];
-      if (id < 0 || id >= c.blocks) continue;
-      const size_t at = ((size_t)id * c.hb + hh) * CB_TOKENS + token % CB_TOKENS;
-      const float* logit = lds + a.kept + (token / CB_TOKENS) * nq * CB_TOKENS + token % CB_TOKENS;
-      float gained = 0.f;                           // small beside what is there: added to it once
-      for (int r = 0; r < nq; ++r) gained += exp2_fast(logit[r * CB_TOKENS] - lse2[r]);   // no token seen: 2^(-inf - inf)
-      a.weight_out[at] = a.weight_in ? a.weight_in[at] + gained : gained;
+    for (int token = tid * 4; token < len; token += CA_THREADS * 4) {
+      const int block = token / CB_TOKENS, in = token % CB_TOKENS;   // four tokens of one block
+      f32x4_t gained{0.f, 0.f, 0.f, 0.f};
+      // a query that sees no token adds nothing: 2^(-inf - inf)
+      const auto add = [&](f32x4_t s, int r) {
+        const float m = lse2[r];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) gained[e] += exp2_fast(s[e] - m);
+      };
+      if (block < a.kept_blocks) {                  // wave-uniform but for the last wave that is in
+        const float* from = lds + a.kept + block * nq * CB_TOKENS + in;
+#pragma unroll 4
+        for (int r = 0; r < nq; ++r) add(*reinterpret_cast<const f32x4_t*>(from + r * CB_TOKENS), r);
+      } else {
+        const float* from = a.logits + (((size_t)b * c.hkv + h) * a.lblocks + block) * a.rows * CB_TOKENS + in;
+#pragma unroll 4
+        for (int r = 0; r < nq; ++r) add(*reinterpret_cast<const f32x4_t*>(from + r * CB_TOKENS), r);
+      }
+      add_weights(a, row, hh, token, len, gained);
     }
   }
 }
@@ -495,17 +525,11 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
   if (chunk * CJ_TOKENS >= len) return;             // uniform
   const int token = chunk * CJ_TOKENS + tid * 4;    // four tokens of one block
   const int n = max(((len + CB_TOKENS - 1) / CB_TOKENS + a.chunk - 1) / a.chunk, 1);
-  const int id = token < len ? c.table[row * c.width + token / CB_TOKENS] : -1;
-  const bool on = id >= 0 && id < c.blocks;
-  const int known = on ? token : 0;
+  const int known = token < len ? token : 0;
   const float* from = a.logits + ((size_t)bh * a.lblocks + known / CB_TOKENS) * a.rows * CB_TOKENS + known % CB_TOKENS;
-  f32x4_t s[CJ_AHEAD];
+  f32x4_t s[CJ_AHEAD], gained{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < CJ_AHEAD; ++i) s[i] = *reinterpret_cast<const f32x4_t*>(from + min(i, a.rows - 1) * CB_TOKENS);
-  const size_t at = ((size_t)(on ? id : 0) * c.hb + cache_head(c, h)) * CB_TOKENS + token % CB_TOKENS;
-  u32x4_word w_in{0, 0, 0, 0};
-  if (on && a.weight_in) w_in = *reinterpret_cast<const u32x4_word*>(a.weight_in + at);
-  float gained[4] = {0.f, 0.f, 0.f, 0.f};
   for (int r0 = 0; r0 < a.rows; r0 += CJ_ROWS) {
     const int most = min(a.rows - r0, CJ_ROWS);
     for (int r = tid / 16; r < most; r += CA_THREADS / 16) {
@@ -532,14 +556,7 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
     }
     __syncthreads();
   }
-  if (!on) return;
-  u32x4_word y;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = __float_as_uint(__uint_as_float(w_in[e]) + gained[e]);
-  float* to = a.weight_out + at;
-  if (token + 4 <= len) *reinterpret_cast<u32x4_word*>(to) = y;
-  else
-    for (int e = 0; e < len - token; ++e) to[e] = __uint_as_float(y[e]);
+  if (token < len) add_weights(a, row, cache_head(c, h), token, len, gained);
 }
 
 // How a call is split.  Two workgroups run on a compute unit, 512 on the chip.  us per call, 32/8 heads of
@@ -552,17 +569,20 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
 //   512 heads and more: whole rows, up to 64 blocks, beyond which one long row among short ones would be
 //     waited for: 64 x 1500 34.1 (24) 41.7 (12); 64 x 6000..12000 192 (whole) 196 (64); 256 x 400..800 59.4 (whole)
 //     115 (4)
-// With weights, where whole rows of a head are one workgroup's work and their logits fit into LDS beside what joins
-// the waves, weights are gathered there and then; else the logits go through the workspace to attend_join.
-// LDS / memory: 64 x 4000 tokens of 32/8 heads (63 KB of logits) 91 / 115 us, of 64/8 heads (126 KB, one
-// workgroup to a compute unit) 116 / 131; 256 x 400..800 68 / 80.  So from 256 heads on rows stay whole where that
-// makes them fit (whole / split): 64 x 8000 218 / 231, 32 x 4000 59 / 65, 32 x 1500 26 / 33; with 128 heads it
-// does not pay: 16 x 4000 46 / 36.
+// With weights, a workgroup that has whole rows of a head gathers them too, from logits that it keeps in LDS beside
+// what joins the waves, and where they do not fit, behind the first blocks', in the workspace, which it reads back while
+// the next workgroup's codes come in; only rows that are split leave that to attend_join.  So from 256 heads on rows
+// of up to 256 blocks stay whole (whole / split, us): 64 x 4000 tokens of 32/8 heads 91 / 115, of 64/8 heads (126 KB of
+// logits, one workgroup to a compute unit) 116 / 131; 32 x 1500 26 / 33; 64 x 8000 218 / 231; 64 x 8192..16384 323 / 360
+// (16 KB of LDS 364, 64 KB 342); 256 x 2800..14000 900 / 1135; 32 x 16384 206 / 229; but short rows only if all
+// their logits fit: 256 x 100..1000 with 32 query rows to a head 175 / 141; and with 128 heads it does not pay: 16 x 4000
+// 46 / 36.
 // The workspace is that of the most splits that any shorter max_length asks for, with its logits.
 constexpr int64_t CA_LDS = 152 << 10;               // of 160 KB
 struct AttendPlan {
   int rows, qt, row_chunks, chunk, splits, lblocks;
-  bool kept;                                        // logits stay in LDS
+  bool kept;                                        // a workgroup gathers the weights of its whole row
+  int kept_blocks;                                  // of it, blocks whose logits stay in LDS
   size_t off_o, off_ml, off_logits, total;
 };
 
@@ -577,13 +597,15 @@ AttendPlan attend_plan(const Problem& pb, int64_t max_length, bool weights) {
   const int64_t least = heads >= 512 ? int64_t(CA_CHUNK_MOST) : heads >= 128 ? 16 : CA_WAVES;
   int64_t chunk = std::min(std::max((nb * heads + target - 1) / target, least), int64_t(CA_CHUNK_MOST));
   if (pb.batch > 1 && chunk < 8 && heads * ((nb + 7) / 8) >= 256) chunk = 8;
-  const bool fits = weights && P.row_chunks == 1 && nb <= 64 * CA_WAVES &&
-                    (nb * CB_TOKENS + CA_WAVES * pb.d) * P.rows * 4 <= CA_LDS;
-  if (fits && heads >= 256) chunk = std::max(chunk, nb);
+  const auto room = [&](int64_t lds) { return (lds / (P.rows * 4) - CA_WAVES * pb.d) / CB_TOKENS; };   // blocks
+  const bool alone = weights && P.row_chunks == 1 && nb <= 64 * CA_WAVES;   // a workgroup could take a whole row
+  const bool fits = alone && nb <= room(CA_LDS);
+  if (alone && heads >= 256 && (fits || nb >= 32)) chunk = std::max(chunk, nb);
   P.chunk = int((chunk + CA_WAVES - 1) / CA_WAVES * CA_WAVES);
   P.splits = int((nb + P.chunk - 1) / P.chunk);
   P.lblocks = int(nb);
-  P.kept = fits && P.splits == 1;
+  P.kept = alone && P.splits == 1 && (fits || nb >= 32);
+  P.kept_blocks = P.kept ? int(std::min(nb, room(CA_LDS))) : 0;
   const size_t all = size_t(pb.batch) * pb.hkv * P.rows;
   // no fewer than splits, whatever nb, and never falling with nb
   const size_t most = size_t(std::min((nb + least - 1) / least,
@@ -603,7 +625,7 @@ template <int FMT, typename T>
 kvc_status attend_form(const Problem& pb, const AttendPlan& P, const AttendArgs& a, unsigned grid, hipStream_t stream) {
   const dim3 g(grid, 1, pb.batch);
   const size_t lds = size_t(CA_WAVES) * std::min(P.rows, 16 * P.qt) * pb.d * 4 +
-                     (P.kept ? size_t(P.lblocks) * P.rows * CB_TOKENS * 4 : 0);
+                     size_t(P.kept_blocks) * P.rows * CB_TOKENS * 4;
 #define KVC_ATTEND(NJ, QT, STREAM)                                                                                        \
   do {                                                                                                                    \
     if (pb.d == 64 * NJ)                                                                                                  \
@@ -652,7 +674,8 @@ kvc_status launch_cache_attend(const Problem& pb, int layer, const void* q, cons
   a.part_o = reinterpret_cast<float*>(base + P.off_o);
   a.part_ml = P.splits > 1 || weights ? reinterpret_cast<float2*>(base + P.off_ml) : nullptr;
   a.kept = P.kept ? CA_WAVES * P.rows * pb.d : 0;
-  a.logits = weights && !P.kept ? reinterpret_cast<float*>(base + P.off_logits) : nullptr;
+  a.kept_blocks = P.kept_blocks;
+  a.logits = weights && P.kept_blocks < P.lblocks ? reinterpret_cast<float*>(base + P.off_logits) : nullptr;
   a.weight_in = weight_in; a.weight_out = weight_out;
   a.c = c;
   a.layer = layer; a.group = pb.group; a.window = pb.window; a.rows = P.rows; a.row_chunks = P.row_chunks;

@@ -199,12 +199,16 @@ def test_random_calls(seed):
           layer=int(rng.integers(0, layers)), weights=str(rng.choice(["add", "set", "none"])), q_size=float(rng.choice([0.3, 1, 4])))
 
 
-def test_weights_of_long_whole_rows():
-    """More than 64 blocks to a workgroup: one query row to a head, rows up to the most that LDS holds."""
-    rng = np.random.default_rng(37)
+@pytest.mark.parametrize("group,window,longest,weights", [(1, 1, 16384, "add"), (4, 1, 14001, "add"), (3, 8, 3001, "set"), (40, 1, 2500, "add"),
+                                                          (2, 1, 16385, "add")])
+def test_weights_of_long_whole_rows(group, window, longest, weights):
+    """More than 64 blocks to a workgroup; logits that LDS holds, that it holds in part, and rows that are split after all."""
+    rng = np.random.default_rng([37, group])
     lens = [int(x) for x in rng.integers(0, 300, 32)]
-    lens[3], lens[30] = 16384, 9001
-    check(rng, random_cache(rng, orc.E4M3, lens, 8, 16, 1), lens, 8)
+    lens[3], lens[30] = longest, longest // 2 + 1
+    c = random_cache(rng, orc.E4M3, lens, 8, 16, 1)
+    c.table[3, [1, -2 - (longest % 64 == 0)]] = -1
+    check(rng, c, lens, 8 * group, window=window, causal=int(window > 1), weights=weights)
 
 
 @pytest.mark.parametrize("batch,hkv,lens", [(64, 8, (1, 300)), (70, 8, (4000, 4400)), (20, 8, (1, 3000)), (9, 8, (500, 2500))])
