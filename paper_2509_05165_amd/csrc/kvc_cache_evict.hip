@@ -38,13 +38,14 @@ __device__ __forceinline__ int kept_tokens(const EvictArgs& a, int64_t row, int 
   return max(min(min(a.keep[row], a.max_keep), len), 0);
 }
 
-// KPT > 0: every key of the row lies in registers, token i * EV_THREADS + tid in key[i].  KPT = 0: longer rows
-// read their weights again in every pass.
-template <int KPT>
-__global__ __launch_bounds__(EV_THREADS, KPT > 0 && KPT <= 16 ? 8 : 4) void evict_select(EvictArgs a) {
+// Rows are worked on EV_THREADS * KPT tokens at a time: those of a row that is no longer stay in registers, token
+// i * EV_THREADS + tid in key[i]; longer ones (LOOP) are read again in every pass, KPT keys in flight per thread.  (256 heads of 30517
+// tokens: 50 us in registers, 104 read again; 60000 tokens 201 us, of 1260 for the eviction.)
+template <int KPT, bool LOOP>
+__global__ __launch_bounds__(EV_THREADS, KPT <= 16 ? 8 : 4) void evict_select(EvictArgs a) {
   __shared__ uint32_t hist[EV_BINS];
   __shared__ uint32_t part[EV_WAVES], found[2];
-  __shared__ uint32_t counts[KPT > 0 ? KPT * EV_WAVES : 2 * EV_WAVES];   // above | equal << 16 of a wave's 64 tokens
+  __shared__ uint32_t counts[KPT * EV_WAVES + 1];   // above | equal << 16 of a wave's 64 tokens; of all
   const CacheView& c = a.c;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   for (int64_t head = blockIdx.x; head < a.heads; head += gridDim.x) {
@@ -70,11 +71,13 @@ __global__ __launch_bounds__(EV_THREADS, KPT > 0 && KPT <= 16 ? 8 : 4) void evic
       const uint32_t key = t < a.keep_first || t >= len - a.keep_last ? EV_FORCED : there ? max(k, 1u) : EV_ABSENT;
       return t < len ? key : 0u;
     };
-    uint32_t key[KPT > 0 ? KPT : 1];
-    if (KPT > 0)
+    uint32_t key[KPT];
+    const auto load = [&](int part) {
 #pragma unroll
-      for (int i = 0; i < KPT; ++i) key[i] = read(i);
-    const int chunks = (len + EV_THREADS - 1) / EV_THREADS;
+      for (int i = 0; i < KPT; ++i) key[i] = read(part * KPT + i);
+    };
+    const int parts = LOOP ? (len + EV_THREADS * KPT - 1) / (EV_THREADS * KPT) : 1;
+    if (!LOOP) load(0);
 
     // ---- the keep-th largest key, digit by digit ----
     uint32_t prefix = 0, mask = 0, left = keep;     // left: to be taken among the keys that match prefix
@@ -86,11 +89,10 @@ __global__ __launch_bounds__(EV_THREADS, KPT > 0 && KPT <= 16 ? 8 : 4) void evic
       const auto count = [&](uint32_t k) {
         if (pass == 0 ? k != 0 : (k & mask) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
       };
-      if (KPT > 0) {
+      for (int s = 0; s < parts; ++s) {
+        if (LOOP) load(s);
 #pragma unroll
         for (int i = 0; i < KPT; ++i) count(key[i]);
-      } else {
-        for (int i = 0; i < chunks; ++i) count(read(i));
       }
       __syncthreads();
       // thread tid holds the bins 2 tid and 2 tid + 1 counted from the top
@@ -130,7 +132,9 @@ __global__ __launch_bounds__(EV_THREADS, KPT > 0 && KPT <= 16 ? 8 : 4) void evic
       const uint32_t at = above + min(equal, left);
       if (take && at < (uint32_t)keep) list[at] = t;
     };
-    if (KPT > 0) {
+    uint32_t above = 0, equal = 0;                  // of all earlier parts
+    for (int s = 0; s < parts; ++s) {
+      if (LOOP) load(s);
 #pragma unroll
       for (int i = 0; i < KPT; ++i) {
         const uint64_t gt = __ballot(key[i] > prefix), eq = __ballot(key[i] == prefix);
@@ -138,7 +142,7 @@ __global__ __launch_bounds__(EV_THREADS, KPT > 0 && KPT <= 16 ? 8 : 4) void evic
       }
       __syncthreads();
       if (wave == 0) {                              // exclusive sums over KPT * 16 entries, KPT / 4 per lane
-        constexpr int PER = KPT > 0 ? KPT / 4 : 1;
+        constexpr int PER = KPT / 4;
         uint32_t mine[PER], incl = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) { mine[i] = counts[lane * PER + i]; incl += mine[i]; }
@@ -148,6 +152,7 @@ __global__ __launch_bounds__(EV_THREADS, KPT > 0 && KPT <= 16 ? 8 : 4) void evic
           const uint32_t o = __shfl_up(incl, off);
           if (lane >= off) incl += o;
         }
+        if (lane == 63) counts[KPT * EV_WAVES] = incl;
         run = incl - run;
 #pragma unroll
         for (int i = 0; i < PER; ++i) { counts[lane * PER + i] = run; run += mine[i]; }
@@ -156,26 +161,12 @@ __global__ __launch_bounds__(EV_THREADS, KPT > 0 && KPT <= 16 ? 8 : 4) void evic
 #pragma unroll
       for (int i = 0; i < KPT; ++i) {
         const uint32_t base = counts[i * EV_WAVES + wave];
-        put(i * EV_THREADS + tid, key[i], base & 0xffff, base >> 16);
+        put((s * KPT + i) * EV_THREADS + tid, key[i], above + (base & 0xffff), equal + (base >> 16));
       }
-    } else {
-      uint32_t above = 0, equal = 0;                // of all earlier chunks
-      for (int i = 0; i < chunks; ++i) {
-        const int t = i * EV_THREADS + tid;
-        const uint32_t k = read(i);
-        const uint64_t gt = __ballot(k > prefix), eq = __ballot(k == prefix);
-        uint32_t* cnt = counts + (i & 1) * EV_WAVES;
-        if (lane == 0) cnt[wave] = __popcll(gt) | __popcll(eq) << 16;
-        __syncthreads();
-        uint32_t all = 0, before = 0;
-#pragma unroll
-        for (int w = 0; w < EV_WAVES; ++w) {
-          if (w < wave) before += cnt[w];
-          all += cnt[w];
-        }
-        put(t, k, above + (before & 0xffff), equal + (before >> 16));
-        above += all & 0xffff;
-        equal += all >> 16;
+      if (LOOP) {
+        above += counts[KPT * EV_WAVES] & 0xffff;
+        equal += counts[KPT * EV_WAVES] >> 16;
+        __syncthreads();                            // counts are free for the next part
       }
     }
     __syncthreads();                                // shared memory is free for the next head
@@ -454,11 +445,12 @@ kvc_status launch_cache_evict(const Problem& pb, const int32_t* lengths, const i
   a.keep_first = pb.keep_first; a.keep_last = pb.keep_last;
   const unsigned grid = (unsigned)std::min<int64_t>(a.heads, 1 << 16);
   const int64_t longest = int64_t(c.width) * CB_TOKENS;
-#define KVC_SELECT(KPT) KVC_LAUNCH("evict_select", stream, evict_select<KPT><<<grid, EV_THREADS, 0, stream>>>(a))
-  if (longest <= 4 * EV_THREADS) KVC_SELECT(4);
-  else if (longest <= 16 * EV_THREADS) KVC_SELECT(16);
-  else if (longest <= 32 * EV_THREADS) KVC_SELECT(32);
-  else KVC_SELECT(0);
+#define KVC_SELECT(KPT, LOOP) \
+  KVC_LAUNCH("evict_select", stream, evict_select<KPT, LOOP><<<grid, EV_THREADS, 0, stream>>>(a))
+  if (longest <= 4 * EV_THREADS) KVC_SELECT(4, false);
+  else if (longest <= 16 * EV_THREADS) KVC_SELECT(16, false);
+  else if (longest <= 32 * EV_THREADS) KVC_SELECT(32, false);
+  else KVC_SELECT(16, true);
 #undef KVC_SELECT
   if (max_keep == 0) return KVC_OK;
   const int blocks = a.lpad / CB_TOKENS;
