@@ -38,9 +38,9 @@ __device__ __forceinline__ int kept_tokens(const EvictArgs& a, int64_t row, int 
   return max(min(min(a.keep[row], a.max_keep), len), 0);
 }
 
-// Rows are worked on EV_THREADS * KPT tokens at a time: those of a row that is no longer stay in registers, token
-// i * EV_THREADS + tid in key[i]; longer ones (LOOP) are read again in every pass, KPT keys in flight per thread.  (256 heads of 30517
-// tokens: 50 us in registers, 104 read again; 60000 tokens 201 us, of 1260 for the eviction.)
+// Rows are worked on EV_THREADS * KPT tokens at a time, token i * EV_THREADS + tid in key[i]: those of a row that is
+// no longer stay in registers; longer ones (LOOP) are read again in every pass, KPT keys in flight per thread.  (256
+// heads of 30517 tokens: 50 us in registers, 104 read again; 60000 tokens 201 us, of 1260 for the eviction.)
 template <int KPT, bool LOOP>
 __global__ __launch_bounds__(EV_THREADS, KPT <= 16 ? 8 : 4) void evict_select(EvictArgs a) {
   __shared__ uint32_t hist[EV_BINS];
@@ -219,7 +219,7 @@ __device__ __forceinline__ float lane_float(float x, int lane) {
 }
 
 // blockDim: 64 * waves, waves = d / 64 rounded up.  magic: 65536 / (d / 16) rounded up.  VALUES: V, else K.
-// Bound by HBM: K 4.9 TB/s, V 4.7 TB/s of the bytes that it moves, which are those of every source block that
+// Bound by HBM: K 5.0 TB/s, V 4.8 TB/s of the bytes that it moves, which are those of every source block that
 // a kept token lies in.
 template <int FMT, bool VALUES>
 __global__ __launch_bounds__(EM_THREADS) void evict_move(EvictArgs a, int blocks, int64_t units, uint32_t magic) {

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(CS_THREADS) void cache_fill(PtrTable k_tab, PtrTabl
                                                          const int32_t* __restrict__ lengths,
                                                          const int64_t* __restrict__ offsets, SeqTable seq,
                                                          CacheView c, int total, int64_t units) {
-  extern __shared__ __align__(16) uint8_t tile[];                // V codes [64][d + 8]
+  extern __shared__ __align__(16) uint8_t tile[];   // V codes [64][d + 8]
   __shared__ float red[2 * CS_THREADS / 64];
   const int d = c.d, pieces = d / 8, stride = d + 8, tid = threadIdx.x;
   const int per_layer = c.hkv / c.hb, rows = seq.batch * c.layers * per_layer;
