@@ -354,8 +354,7 @@ kvc_status kvc_cache_append(const kvc_params* params, int32_t layer, const void*
  * A query that sees no token gives out = 0 and lse = -infinity.  Values of V beyond 2^90 in size may
  * overflow in the sums.  Products on the bf16 matrix cores
  * with fp32 accumulation: codes are bf16 numbers exactly; for the product with V bf16 calls round
- * probabilities to two bf16 terms (to one where G * M > 16 and d <= 128), fp32 calls split queries and
- * probabilities into three. */
+ * probabilities to two bf16 terms (16 bits), fp32 calls split queries and probabilities into three. */
 kvc_status kvc_cache_attend(const kvc_params* params, int32_t layer, const void* q,
                             const int32_t* lengths, int64_t max_length, const kvc_cache* cache,
                             void* out, float* lse, const float* weight_in, float* weight_out,

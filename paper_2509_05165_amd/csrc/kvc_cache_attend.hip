@@ -7,9 +7,8 @@
 // Codes of both formats are bf16 numbers exactly, so both products run on the bf16 matrix cores with
 // fp32 accumulation; the scales are applied to the fp32 logits and to the fp32 probabilities
 // (exactly, they are powers of two).  For the second product bf16 calls round the probabilities to two bf16
-// terms, 16 bits, or, with more than 16 query rows to a KV head, to one (half a step, 2^-8 relative, as much as the
-// output's own rounding); float32 calls split queries and probabilities into three terms each, 24
-// bits, and lose nothing.
+// terms, 16 bits, so that only the output's own rounding counts; float32 calls split queries and probabilities
+// into three terms each, 24 bits.
 //
 // Layout: v_mfma_f32_16x16x32_bf16 with tokens on the rows and queries on the columns of the first
 // product.  A wave takes a block of 64 tokens as four tiles; tile t holds the tokens 16*g + 4*t + i
@@ -174,12 +173,15 @@ __device__ __forceinline__ void add_weights(const AttendArgs& a, int64_t row, in
 // as this block's output is.
 template <int FMT, typename T, int NJ, bool EXACT, int QT, bool STREAM>
 __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void attend_split(AttendArgs a) {
-  // Terms of the queries and of the probabilities.  bf16 calls: queries are one term; a second one for the
-  // probabilities (16 bits) is free where the codes bound the kernel (64 x 16k tokens, 32/8 heads 335.9 us with one, 338.7
-  // with two; output error against float64 2.4e-3 -> 1.7e-3, its own rounding) and costs where 32 rows share them
-  // (M = 8: 433 / 484).
-  constexpr int TERMS = sizeof(T) == 2 ? 1 : 3, PTERMS = sizeof(T) == 2 ? (QT == 1 ? 2 : 1) : 3;
+  // Terms of the queries and of the probabilities.  bf16 calls: queries are one term, probabilities two whatever the
+  // shape (16 bits; output error against float64 1.7e-3, its own rounding; 2.4e-3 with one).  That is free where the codes
+  // bound the kernel (64 x 16k tokens, 32/8 heads 335.9 us with one, 338.7 with two) and costs where 32 rows share them:
+  // 64 x 8k..16k tokens 357 / 372 with 8 query tokens, 16 x 8k..16k 395 / 469 with 64.
+  constexpr int TERMS = sizeof(T) == 2 ? 1 : 3, PTERMS = sizeof(T) == 2 ? 2 : 3;
   constexpr int NT = 4 * NJ;                        // tiles of 16 dimensions
+  // Two tiles of bf16 queries lie in LDS, where the waves join their results later (it has room for them: 17 rows or
+  // more of d floats from every wave): in registers 26 others were spilled (8 query tokens, as above: 416 us).
+  constexpr bool Q_LDS = QT == 2 && sizeof(T) == 2;
   extern __shared__ __align__(16) float lds[];      // [waves][nq][d], nq = query rows of this workgroup; at kept [kept_blocks][nq][64]
   __shared__ float sm[CA_WAVES][16 * QT], sl[CA_WAVES][16 * QT], lse2[16 * QT];
   const CacheView& c = a.c;
@@ -247,8 +249,9 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
     load_v(id);
   }
 
-  // ---- queries: lane col holds row col, dimensions 64 j + 16 g + 8 half ----
+  // ---- queries: lane col holds row col, dimensions 64 j + 16 g + 8 half (q_lds: its own 16 bytes of every piece) ----
   bf16x8_t q[QT][NJ][2][TERMS];
+  u32x4_t* const q_lds = reinterpret_cast<u32x4_t*>(lds) + lane;
   int limit[QT];                                    // tokens that the lane's query sees
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -265,8 +268,11 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
         float f[8];
         w.get(f);
         split_terms<TERMS>(f, q[t][j][half]);
+        const int piece = (t * NJ + j) * 2 + half;  // the waves hold the same queries: each stores some
+        if (Q_LDS && piece % CA_WAVES == wave) q_lds[piece * 64] = __builtin_bit_cast(u32x4_t, q[t][j][half][0]);
       }
   }
+  if (Q_LDS) __syncthreads();
 
   f32x4_t o[QT][NT];
   float ref[QT], sum[QT];
@@ -296,6 +302,10 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
+        bf16x8_t qf[QT];
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt)
+          if (Q_LDS) qf[qt] = __builtin_bit_cast(bf16x8_t, q_lds[((qt * NJ + j) * 2 + half) * 64]);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const bf16x8_t kf = Code<FMT>::widen(operand(t, j, 2 * half), operand(t, j, 2 * half + 1));
@@ -303,7 +313,7 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
           for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
             for (int n = TERMS - 1; n >= 0; --n)
-              s[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[qt][j][half][n], s[qt][t], 0, 0, 0);
+              s[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, Q_LDS ? qf[qt] : q[qt][j][half][n], s[qt][t], 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);          // no more than one step's widened codes in registers
       }

@@ -92,3 +92,42 @@ def attend_tolerance(c, q, mean_abs, largest, out, dtype):
     half = torch.finfo(DTYPES[dtype][0]).eps / 2
     p = half if dtype == "bf16" else 2.0 ** -23
     return mean_abs * (2 * rel[..., None] + p) * 1.01 + np.abs(out) * half + 1e-37
+
+
+def attend_bounds(c, lens, mean_abs, largest, out, lse, dtype):
+    """Largest errors of the outputs and of the log-sum-exps, counted by how sums are added up: a wave adds 16
+    probabilities of a block per lane and then the blocks that are its own, at most 64 of a row that one workgroup takes and 16 of
+    a longer one; a product of the matrix cores adds 32 terms to its accumulator, one after the other at worst; the
+    waves (4) and the splits (at most 128 in a chain) come last.  Every addition is off by a step, 2^-23, at most (the matrix
+    cores need not round).  Logits are d products of `terms` parts, scaled, taken from the reference and
+    turned into log2 units; the exponential is within 2 ulp; probabilities of the second product are held in 16
+    bits by bf16 calls, in 24 by fp32 ones.  out is rounded once, to half a step of its type."""
+    u, bf16 = 2.0 ** -23, dtype == "bf16"
+    terms, parts = (1, 2) if bf16 else (3, 3)
+    blocks = -(-max(max(lens), 1) // 64)
+    deep = min(blocks, 64) if blocks <= 256 else 16
+    joins = 4 + (128 if blocks > 4 else 0)
+    rel = largest * u * (terms * (c.d + 2) + 4) + 2 * u
+    sums = (16 + 2 * deep + 2 + joins) * u
+    products = (deep * (2 * parts * 32 + 1) + joins) * u
+    half = torch.finfo(DTYPES[dtype][0]).eps / 2
+    p = 2.0 ** -16 if bf16 else 2.0 ** -24
+    tol = mean_abs * (2 * rel[..., None] + sums + products + p) + np.abs(out) * half + 1e-37
+    return tol, rel + sums + np.abs(np.where(np.isfinite(lse), lse, 0)) * 2 * u
+
+
+def call_attend(c, q, lens, dtype, causal=0, scale=0.0, max_length=None, layer=0, weights=True):
+    """out, lse and weight_out (7 where nothing is written) of one call, in float64."""
+    batch, hq, window, _ = q.shape
+    device, lengths, tq = Device(c), dev(np.asarray(lens, np.int32)), dev(q, dtype)
+    out, lse = torch.full_like(tq, 7.0), torch.full(q.shape[:3], 7.0, device="cuda")
+    gathered = torch.full(c.weight.shape, 7.0, device="cuda")
+    p = params(c, batch, hq, dtype, window, causal_tail=causal, softmax_scale=scale)
+    most = max(lens) if max_length is None else max_length
+    size = kv.kvc_cache_attend_workspace(p, most, weights)
+    ws = workspace(size)
+    kv.kvc_cache_attend(p, layer, tq.data_ptr(), lengths.data_ptr(), most, device.struct, out.data_ptr(), ws.data_ptr(), size,
+                        stream(), lse=lse.data_ptr(), weight_in=device.t["weight"].data_ptr() if weights else 0,
+                        weight_out=gathered.data_ptr() if weights else 0)
+    device.same(c)
+    return tuple(x.double().cpu().numpy() for x in (out, lse, gathered))

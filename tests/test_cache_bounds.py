@@ -1,0 +1,34 @@
+"""What the error bounds of the attention tests can see: mistakes planted in the oracle lie outside them."""
+import numpy as np
+import pytest
+
+from cache_testlib import attend_bounds, random_cache, rounded
+from oracle import cache_oracle as orc
+from test_gpu_cache_precision import few_tokens
+
+
+def bf16(x):
+    return rounded(x, "bf16")
+
+
+def rows_of(c, lens, q, scale, terms):
+    """Attention with probabilities, in units of the largest one, held in `terms` bf16 terms for the product with V alone."""
+    out, group = np.zeros(q.shape), q.shape[1] // c.hkv
+    for row, hh, b, _, h in c.heads():
+        k, v, _, _ = c.tokens(row, hh, lens[row])
+        for g in range(h * group, (h + 1) * group):
+            s = (q[b, g] @ k.T) * scale
+            e = np.exp(s - s.max(axis=1, keepdims=True))
+            held = bf16(e)
+            held = held + bf16(e - held) if terms == 2 else held
+            out[b, g] = bf16(held @ v / e.sum(axis=1, keepdims=True))
+    return out
+
+
+@pytest.mark.parametrize("group,window,d,fmt", [(4, 8, 64, orc.E4M3), (5, 4, 128, orc.INT8), (1, 1, 64, orc.INT8)])
+def test_probabilities_of_eight_bits(group, window, d, fmt):
+    c, lens, q = few_tokens(fmt, d, group, window)
+    out, lse, _, mean_abs, largest = orc.attend(c, 0, q, lens, d ** -0.5)
+    tol, _ = attend_bounds(c, lens, mean_abs, largest, out, lse, "bf16")
+    assert (np.abs(rows_of(c, lens, q, d ** -0.5, 2) - out) <= tol).all()
+    assert (np.abs(rows_of(c, lens, q, d ** -0.5, 1) - out) > tol).mean() > 0.02
