@@ -352,7 +352,7 @@ kvc_status kvc_cache_append(const kvc_params* params, int32_t layer, const void*
  *               weight_out[c] = weight_in[c] + sum over the M queries and the G heads of its KV
  *               head of the probability of c.  weight_in NULL counts as 0; both may be the cache's weight.
  * A query that sees no token gives out = 0 and lse = -infinity.  Values of V beyond 2^90 in size may
- * overflow in the sums.  Products on the bf16 matrix cores
+ * overflow in out; what a block of V adds to out has fewer bits where probability * scale is below 2^-126.  Products on the bf16 matrix cores
  * with fp32 accumulation: codes are bf16 numbers exactly; for the product with V bf16 calls round
  * probabilities to two bf16 terms (16 bits), fp32 calls split queries and probabilities into three. */
 kvc_status kvc_cache_attend(const kvc_params* params, int32_t layer, const void* q,

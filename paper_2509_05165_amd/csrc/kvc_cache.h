@@ -17,7 +17,7 @@
 namespace kvc {
 
 constexpr int CB_TOKENS = 64;          // tokens of a block
-constexpr int CB_SCALE_MIN = -100;     // least exponent of a scale: p * scale in the products stays normal
+constexpr int CB_SCALE_MIN = -100;     // least exponent of a scale: it and its inverse are normal numbers, and code * scale too
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));

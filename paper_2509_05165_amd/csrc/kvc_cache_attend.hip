@@ -36,6 +36,12 @@ constexpr int CA_CHUNK_MOST = 64;                   // blocks of a workgroup, se
 // A reference further than this below the largest logit is moved up (log2 units): sums stay below
 // 2^8 * 2^30 and rescaling is rare.
 constexpr float CA_SLACK = 8.0f;
+// The scale of V goes into the exponential of the probabilities, which costs nothing, as long as it lies between these:
+// at 2^-60 numbers stay normal down to p = 2^-66, so that the sum of a row misses nothing whatever its values; a
+// block of zeros has the scale 2^-100, where all p below 2^-26 would be missing.  What is left of a smaller or larger
+// scale multiplies the operand of the product with V alone (always multiplying there: 64 x 8k..16k tokens, heads of 64,
+// 8 query tokens 223 us instead of 204).
+constexpr float CA_EXP_LEAST = 0x1p-60f, CA_EXP_MOST = 0x1p60f;
 
 struct AttendArgs {
   const void* q;
@@ -321,8 +327,9 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
     const int here = id < 0 ? 0 : len;              // tokens of an absent block are masked like those past the end
     const int first = p * CB_TOKENS + 16 * g;       // the lane's 16 tokens
     const bool tail = (p + 1) * CB_TOKENS > here - (a.causal ? a.window - 1 : 0);   // wave-uniform
-    const float shift = __builtin_amdgcn_logf(vs);  // whole: vs is a power of two
-    const float inv_vs = inverse_scale(vs);
+    const float in_exp = fminf(fmaxf(vs, CA_EXP_LEAST), CA_EXP_MOST);   // of vs, what the exponential takes
+    const float shift = __builtin_amdgcn_logf(in_exp);   // whole: a power of two
+    const float inv_exp = inverse_scale(in_exp);
     bf16x8_t pf[QT][2][PTERMS];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
@@ -360,7 +367,7 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
 #pragma unroll
         for (int n = 0; n < NT; ++n) o[qt][n] *= f;
       }
-      // p * vs = 2^(s ks - ref + log2 vs); no token seen yet: 2^(-inf - 0) = 0
+      // p * in_exp = 2^(s ks - ref + log2 in_exp); no token seen yet: 2^(-inf - 0) = 0
       const float base = shift - (ref[qt] == -INFINITY ? 0.f : ref[qt]);
       float pr[2][8], part = 0.f;
 #pragma unroll
@@ -371,7 +378,12 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
           part += e;
           pr[t >> 1][4 * (t & 1) + i] = e;
         }
-      sum[qt] = fmaf(part, inv_vs, sum[qt]);
+      sum[qt] = fmaf(part, inv_exp, sum[qt]);
+      if (in_exp != vs)                             // uniform
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) pr[u][i] *= vs * inv_exp;
 #pragma unroll
       for (int u = 0; u < 2; ++u) split_terms<PTERMS>(pr[u], pf[qt][u]);
     }

@@ -94,12 +94,12 @@ def attend_tolerance(c, q, mean_abs, largest, out, dtype):
     return mean_abs * (2 * rel[..., None] + p) * 1.01 + np.abs(out) * half + 1e-37
 
 
-def attend_bounds(c, lens, mean_abs, largest, out, lse, dtype):
+def attend_bounds(c, lens, mean_abs, largest, out, lse, dtype, dims=None):
     """Largest errors of the outputs and of the log-sum-exps, counted by how sums are added up: a wave adds 16
     probabilities of a block per lane and then the blocks that are its own, at most 64 of a row that one workgroup takes and 16 of
     a longer one; a product of the matrix cores adds 32 terms to its accumulator, one after the other at worst; the
     waves (4) and the splits (at most 128 in a chain) come last.  Every addition is off by a step, 2^-23, at most (the matrix
-    cores need not round).  Logits are d products of `terms` parts, scaled, taken from the reference and
+    cores need not round).  Logits are d products (`dims` of them not 0) of `terms` parts, scaled, taken from the reference and
     turned into log2 units; the exponential is within 2 ulp; probabilities of the second product are held in 16
     bits by bf16 calls, in 24 by fp32 ones.  out is rounded once, to half a step of its type."""
     u, bf16 = 2.0 ** -23, dtype == "bf16"
@@ -107,7 +107,7 @@ def attend_bounds(c, lens, mean_abs, largest, out, lse, dtype):
     blocks = -(-max(max(lens), 1) // 64)
     deep = min(blocks, 64) if blocks <= 256 else 16
     joins = 4 + (128 if blocks > 4 else 0)
-    rel = largest * u * (terms * (c.d + 2) + 4) + 2 * u
+    rel = largest * u * (terms * ((dims or c.d) + 2) + 4) + 2 * u
     sums = (16 + 2 * deep + 2 + joins) * u
     products = (deep * (2 * parts * 32 + 1) + joins) * u
     half = torch.finfo(DTYPES[dtype][0]).eps / 2

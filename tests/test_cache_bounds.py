@@ -2,9 +2,9 @@
 import numpy as np
 import pytest
 
-from cache_testlib import attend_bounds, random_cache, rounded
+from cache_testlib import attend_bounds, rounded
 from oracle import cache_oracle as orc
-from test_gpu_cache_precision import few_tokens
+from test_gpu_cache_precision import far_below, few_tokens
 
 
 def bf16(x):
@@ -32,3 +32,15 @@ def test_probabilities_of_eight_bits(group, window, d, fmt):
     tol, _ = attend_bounds(c, lens, mean_abs, largest, out, lse, "bf16")
     assert (np.abs(rows_of(c, lens, q, d ** -0.5, 2) - out) <= tol).all()
     assert (np.abs(rows_of(c, lens, q, d ** -0.5, 1) - out) > tol).mean() > 0.02
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_sum_without_small_probabilities(dtype):
+    c, lens, q = far_below(orc.INT8, (1 << 19) - 5, -100, 0)
+    q = rounded(q, dtype)
+    out, lse, _, mean_abs, largest = orc.attend(c, 0, q, lens, 1.0)
+    short, short_lse, _, _, _ = orc.attend(c, 0, q, [64], 1.0)               # all but the first block are missing
+    tol, tol_lse = attend_bounds(c, lens, mean_abs, largest, out, lse, dtype)
+    assert (np.abs(short_lse - lse) > 4 * tol_lse).all()
+    if dtype == "f32":
+        assert (np.abs(short - out) > tol)[..., 1::2].all()

@@ -30,3 +30,60 @@ def test_probabilities_have_sixteen_bits(fmt, d, group, window):
         print("largest share of the bound", share.max(), flush=True)
         assert (share <= 1).all()
         assert (np.abs(mine_lse - lse) <= tol_lse).all()
+
+
+def far_below(fmt, n, scale_exponent, code, first_exponent=-4, units=27, hkv=1):
+    """A first token whose probability is 2^units times that of every other one; behind its block, values of one code
+    under one scale.  Every other dimension of the first block's values is 0."""
+    d, blocks = 16, -(-n // 64)
+    c = orc.Cache(fmt, blocks + 1, hkv, d, [np.random.default_rng(71).permutation(blocks + 1)[:blocks]], 1)
+    c.k_scale[:], c.v_scale[:], c.weight[:] = 1, np.float32(2.0 ** scale_exponent), 0
+    c.v[:] = code
+    first = int(c.table[0, 0])
+    c.v[first] = orc.encode(np.random.default_rng(72).uniform(-100, 100, (hkv, d, 64)) * (np.arange(d) % 2)[:, None], fmt)
+    c.v_scale[first] = np.float32(2.0 ** first_exponent)
+    c.k[first, :, 0, 0] = orc.encode(1.0, fmt)
+    q = np.zeros((1, 2 * hkv, 1, d))
+    q[:, :, :, 0] = units * np.log(2.0)
+    return c, [n], q
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale_exponent,code,first,units", [
+    (-100, 0, -4, 27), (-100, 1, -4, 27), (-90, 3, -4, 27), (-59, 3, -4, 27), (0, 0, -4, 27), (70, 1, -4, 27),
+    (-100, 90, -100, 27), (-100, 90, -100, 36), (-95, 90, -95, 36), (61, 90, 61, 36)])
+def test_tokens_count_whatever_the_size_of_their_values(fmt, dtype, scale_exponent, code, first, units):
+    """Half a million tokens far below the first one: at 2^-27 they have 2^-8 of the sum between them, and every other
+    dimension of the output is theirs alone."""
+    c, lens, q = far_below(fmt, (1 << 19) - 5, scale_exponent, code, first, units)
+    q = rounded(q, dtype)
+    out, lse, got, mean_abs, largest = orc.attend(c, 0, q, lens, 1.0)
+    tol, tol_lse = attend_bounds(c, lens, mean_abs, largest, out, lse, dtype)
+    for weights in (True, False):
+        mine, mine_lse, gathered = call_attend(c, q, lens, dtype, scale=1.0, weights=weights)
+        print("lse", mine_lse.ravel(), lse.ravel(), "largest share of the bound", (np.abs(mine - out) / tol).max(), flush=True)
+        assert (np.abs(mine_lse - lse) <= tol_lse).all()
+        assert (np.abs(mine - out) <= tol).all()
+        if weights:
+            # the first token's own weight: the sum's relative error and its rounding
+            assert abs(gathered[c.table[0, 0], 0, 0] - got[0, 0][0]) <= got[0, 0][0] * (2 * tol_lse.max() + 2.0 ** -23)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("scale_exponent,units", [(-100, 20), (-100, 27), (-100, 29), (-95, 32), (-90, 37), (-64, 37), (70, 34)])
+def test_small_values_keep_the_bits_of_their_probabilities(fmt, scale_exponent, units):
+    """p * scale about and below the least normal number, in dimensions that are the small tokens' alone; heads enough for
+    a wave to have several blocks, so that three of sixteen are behind the large token."""
+    c, lens, q = far_below(fmt, 1024, scale_exponent, 90, scale_exponent, units, 128)
+    q = rounded(q, "f32")
+    out, lse, got, mean_abs, largest = orc.attend(c, 0, q, lens, 1.0)
+    tol, tol_lse = attend_bounds(c, lens, mean_abs, largest, out, lse, "f32", dims=1)
+    codes = np.abs(c.tokens(0, 0, 1024)[1]).sum(axis=0) * 2.0 ** -scale_exponent
+    tol += codes * 2.0 ** -133                        # below the normal numbers p * scale is whole steps of bf16's least one
+    for weights in (False, True):
+        mine, mine_lse, gathered = call_attend(c, q, lens, "f32", scale=1.0, weights=weights)
+        print("largest share of the bound", (np.abs(mine - out) / tol).max(), flush=True)
+        assert (np.abs(mine - out) <= tol).all() and (np.abs(mine_lse - lse) <= tol_lse).all()
