@@ -346,11 +346,13 @@ kvc_status kvc_cache_append(const kvc_params* params, int32_t layer, const void*
  * [Bt, Hq, M, d].  Every query sees all tokens of its row or, with causal_tail = 1, query m the
  * first lengths[row] - M + 1 + m (the queries are the row's last M tokens).  Scale: softmax_scale.
  *   max_length  host: no row is read beyond so many tokens (sizes the launch and the workspace;
- *               what exceeds the table counts as the table's capacity)
+ *               what exceeds the table counts as the table's capacity).  The causal tail stays where
+ *               lengths[row] puts it: of the tokens that a query sees, those below max_length count
  *   lse         device float [Bt, Hq, M] or NULL: logarithm of the sum of exp(logits)
  *   weight_out  device, laid out as the cache's weight, or NULL: for every token c of the row
  *               weight_out[c] = weight_in[c] + sum over the M queries and the G heads of its KV
  *               head of the probability of c.  weight_in NULL counts as 0; both may be the cache's weight.
+ * Tokens from max_length on and those of absent blocks are left out of weight_out too (not written).
  * A query that sees no token gives out = 0 and lse = -infinity.  Values of V beyond 2^90 in size may
  * overflow in out; what a block of V adds to out has fewer bits where probability * scale is below 2^-126.  Products on the bf16 matrix cores
  * with fp32 accumulation: codes are bf16 numbers exactly; for the product with V bf16 calls round
@@ -359,7 +361,7 @@ kvc_status kvc_cache_attend(const kvc_params* params, int32_t layer, const void*
                             const int32_t* lengths, int64_t max_length, const kvc_cache* cache,
                             void* out, float* lse, const float* weight_in, float* weight_out,
                             void* workspace, size_t workspace_bytes, void* stream);
-/* Bytes of workspace of such a call; weights: 1 if weight_out is given. */
+/* Bytes of workspace of such a call, max_length < 2^29 (no table holds more); weights: 1 if weight_out is given. */
 kvc_status kvc_cache_attend_workspace(const kvc_params* params, int64_t max_length, int32_t weights,
                                       size_t* bytes);
 

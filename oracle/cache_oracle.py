@@ -172,12 +172,13 @@ def attend(cache, layer, q, lengths, scale, causal=False, max_length=1 << 29):
     for row, hh, b, l, h in cache.heads():
         if l != layer:
             continue
-        n = min(cache.length(lengths[row]), max_length)
+        whole = cache.length(lengths[row])
+        n = min(whole, max_length)
         k, v, _, there = cache.tokens(row, hh, n)
         got = np.zeros(n)
         for g in range(h * group, (h + 1) * group):
             for j in range(m):
-                seen = there & (np.arange(n) < (n - m + 1 + j if causal else n))
+                seen = there & (np.arange(n) < (whole - m + 1 + j if causal else n))
                 if not seen.any():
                     continue
                 s = (k[seen] @ q[b, g, j]) * scale

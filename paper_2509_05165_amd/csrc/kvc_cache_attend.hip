@@ -202,7 +202,7 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
   // (a chunk has at most 64 * CA_WAVES blocks)
   const int my_block = first_block + CA_WAVES * lane;
   int my_id = c.table[row * c.width + min(my_block, c.width - 1)];
-  const int len = attend_length(a, row);
+  const int whole_len = cache_length(c, a.lengths[row]), len = min(whole_len, a.max_length);
   const int nb = (len + CB_TOKENS - 1) / CB_TOKENS;
   const int hi = min(lo + a.chunk, nb);
   if (split > 0 && lo >= nb) return;                // attend_join knows that this split is empty
@@ -258,11 +258,11 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
   // ---- queries: lane col holds row col, dimensions 64 j + 16 g + 8 half (q_lds: its own 16 bytes of every piece) ----
   bf16x8_t q[QT][NJ][2][TERMS];
   u32x4_t* const q_lds = reinterpret_cast<u32x4_t*>(lds) + lane;
-  int limit[QT];                                    // tokens that the lane's query sees
+  int limit[QT];                                    // tokens that the lane's query sees (of them, those below len are read)
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const int r = t * 16 + col;
-    limit[t] = a.causal && r < nq ? len - (a.window - 1 - (r0 + r) % a.window) : len;
+    limit[t] = a.causal && r < nq ? whole_len - (a.window - 1 - (r0 + r) % a.window) : len;
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll

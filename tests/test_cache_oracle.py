@@ -83,3 +83,22 @@ def test_eviction_by_hand():
     np.testing.assert_array_equal(orc.decode(c.k[2, 0, :5, 0], orc.INT8) * c.k_scale[2, 0], [2, 4, 5, 6, 0])
     np.testing.assert_array_equal(orc.decode(c.v[2, 0, 3, :5], orc.INT8) * c.v_scale[2, 0], [-2, -4, -5, -6, 0])
     np.testing.assert_array_equal(c.weight[2, 0, :5], np.array([.5, .5, .5, 0, 0], np.float32))
+
+
+@pytest.mark.parametrize("most", [1, 40, 93, 95, 97, 100, 130])
+def test_a_causal_tail_stays_where_the_length_puts_it(most):
+    """Query m sees the first length - M + 1 + m tokens, of which those below max_length are read."""
+    rng = np.random.default_rng(5)
+    c = random_cache(rng, orc.INT8, [100], 1, 16, 1)
+    q = rng.standard_normal((1, 1, 6, 16))
+    out, lse, got, _, _ = orc.attend(c, 0, q, [100], 0.25, causal=True, max_length=most)
+    k, v, _, _ = c.tokens(0, 0, 100)
+    gathered = np.zeros(min(100, most))
+    for m in range(6):
+        n = min(100 - 6 + 1 + m, most)
+        s = torch.from_numpy(k[:n] @ q[0, 0, m] * 0.25)
+        p = torch.softmax(s, 0).numpy()
+        np.testing.assert_allclose(out[0, 0, m], p @ v[:n], atol=1e-13)
+        np.testing.assert_allclose(lse[0, 0, m], torch.logsumexp(s, 0).numpy(), atol=1e-13)
+        gathered[:n] += p
+    np.testing.assert_allclose(got[0, 0], gathered, atol=1e-13)
