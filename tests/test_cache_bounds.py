@@ -4,7 +4,7 @@ import pytest
 
 from cache_testlib import attend_bounds, rounded
 from oracle import cache_oracle as orc
-from test_gpu_cache_precision import far_below, few_tokens
+from test_gpu_cache_precision import far_below, few_tokens, many_tokens
 
 
 def bf16(x):
@@ -44,3 +44,47 @@ def test_a_sum_without_small_probabilities(dtype):
     assert (np.abs(short_lse - lse) > 4 * tol_lse).all()
     if dtype == "f32":
         assert (np.abs(short - out) > tol)[..., 1::2].all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_missing_blocks_of_a_million_tokens(dtype):
+    c, lens, q = many_tokens()
+    q = rounded(q, dtype)
+
+    def run(x, n):
+        return orc.attend(x, 0, q, [n], 1.0)
+
+    def without(first, count):
+        x = c.copy()
+        x.table[0, first:first + count] = -1
+        return run(x, lens[0])
+
+    out, lse, got, mean_abs, largest = run(c, lens[0])
+    tol, tol_lse = attend_bounds(c, lens, mean_abs, largest, out, lse, dtype)
+    assert 0.01 < got[0, 0][-17:].sum() / 2 < 0.05
+    few = 1 if dtype == "bf16" else 2                                           # blocks that the log-sum-exp shows
+    for first in (0, 7777, 16382):
+        assert (np.abs(without(first, few)[1] - lse) > tol_lse).all()
+    for first in (0, 7200, 16344):                                              # what one workgroup takes: the outputs too
+        other = without(first, 36)
+        assert (np.abs(other[0] - out) > tol).mean() > 0.5 and (np.abs(other[1] - lse) > 10 * tol_lse).all()
+    end = run(c, lens[0] - 17)
+    assert (np.abs(end[0] - out) > tol).mean() > 0.8 and (np.abs(end[1] - lse) > 10 * tol_lse).all()
+    assert (np.abs(out) > tol).mean() > 0.9                                     # all zeros
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_missing_blocks_of_an_ordinary_row(dtype):
+    """Without one of its 24 blocks."""
+    c, lens, q = many_tokens(1500, 0)
+    q = rounded(q, dtype)
+    out, lse, _, mean_abs, largest = orc.attend(c, 0, q, lens, 1.0)
+    tol, tol_lse = attend_bounds(c, lens, mean_abs, largest, out, lse, dtype)
+    for block in (0, 11, 22):
+        x = c.copy()
+        x.table[0, block] = -1
+        other = orc.attend(x, 0, q, lens, 1.0)
+        assert (np.abs(other[1] - lse) > 10 * tol_lse).all()
+        if dtype == "f32":                                                      # (bf16: beside a step of the output)
+            assert (np.abs(other[0] - out) > tol).mean() > 0.5
+    assert (np.abs(out) > tol).mean() > 0.9

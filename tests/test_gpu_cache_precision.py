@@ -87,3 +87,59 @@ def test_small_values_keep_the_bits_of_their_probabilities(fmt, scale_exponent, 
         mine, mine_lse, gathered = call_attend(c, q, lens, "f32", scale=1.0, weights=weights)
         print("largest share of the bound", (np.abs(mine - out) / tol).max(), flush=True)
         assert (np.abs(mine - out) <= tol).all() and (np.abs(mine_lse - lse) <= tol_lse).all()
+
+
+def many_tokens(n=(1 << 20) + 17, end=112):
+    """A row whose values differ from one stretch of 36 blocks to the next, and whose last 17 tokens (codes of `end`) have a
+    fiftieth of the probability between them: a missing block, stretch or end shows."""
+    rng = np.random.default_rng(73)
+    d, blocks = 16, -(-n // 64)
+    c = orc.Cache(orc.INT8, blocks + 3, 1, d, [rng.permutation(blocks + 3)[:blocks]], 1)
+    c.k_scale[:], c.v_scale[:] = 2.0 ** -5, 2.0 ** -6
+    c.weight[:] = rng.random(c.weight.shape, dtype=np.float32) ** 4
+    at = c.table[0]
+    c.k[at] = rng.integers(-8, 9, (blocks, 1, 64, d)).astype(np.int8).view(np.uint8)
+    mean = rng.integers(-90, 91, (-(-blocks // 36), 1, d, 1))[np.arange(blocks) // 36]
+    c.v[at] = (mean + rng.integers(-20, 21, (blocks, 1, d, 64))).astype(np.int8).view(np.uint8)
+    c.k[at[-1], 0, :17, 0] = end
+    q = rng.standard_normal((1, 2, 1, d)) * 0.5
+    q[..., 0] = 2
+    return c, [n], q
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("weights", [False, True])
+def test_every_block_of_a_million_tokens(dtype, weights):
+    c, lens, q = many_tokens()
+    q = rounded(q, dtype)
+    out, lse, got, mean_abs, largest = orc.attend(c, 0, q, lens, 1.0)
+    tol, tol_lse = attend_bounds(c, lens, mean_abs, largest, out, lse, dtype)
+    mine, mine_lse, gathered = call_attend(c, q, lens, dtype, scale=1.0, weights=weights)
+    print("largest share of the bounds", (np.abs(mine - out) / tol).max(), (np.abs(mine_lse - lse) / tol_lse).max(), flush=True)
+    assert (np.abs(mine - out) <= tol).all()
+    assert (np.abs(mine_lse - lse) <= tol_lse).all()
+    if weights:
+        n, at = lens[0], c.table[0]
+        want = c.weight[at, 0].astype(np.float64).ravel()[:n] + got[0, 0]
+        mine = gathered[at, 0].ravel()
+        # a probability is as far off as its logit and the log-sum-exp; then the sum over the heads, and with the old weight
+        assert (np.abs(mine[:n] - want) <= got[0, 0] * (2 * tol_lse.max() + 2.0 ** -22) + want * 2.0 ** -23).all()
+        assert (mine[n:] == 7).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("lens,hkv,group,window,d", [([1500, 300], 2, 2, 2, 64), ([900, 64, 65], 4, 8, 4, 128), ([700] * 3, 1, 5, 1, 80),
+                                                     ([400] * 40, 8, 4, 1, 32), ([2100, 63], 2, 1, 40, 256)])
+def test_ordinary_rows(fmt, dtype, lens, hkv, group, window, d):
+    rng = np.random.default_rng([75, d, fmt])
+    c = random_cache(rng, fmt, lens, hkv, d, 1)
+    q = rounded(rng.standard_normal((len(lens), hkv * group, window, d)), dtype)
+    out, lse, _, mean_abs, largest = orc.attend(c, 0, q, lens, d ** -0.5, causal=window > 1)
+    tol, tol_lse = attend_bounds(c, lens, mean_abs, largest, out, lse, dtype)
+    for weights in (False, True):
+        mine, mine_lse, _ = call_attend(c, q, lens, dtype, causal=int(window > 1), weights=weights)
+        print("largest share of the bounds", (np.abs(mine - out) / tol).max(), flush=True)
+        assert (np.abs(mine - out) <= tol).all() and (np.abs(mine_lse - lse) <= tol_lse).all()
