@@ -185,9 +185,10 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
   // 64 x 8k..16k tokens 357 / 372 with 8 query tokens, 16 x 8k..16k 395 / 469 with 64.
   constexpr int TERMS = sizeof(T) == 2 ? 1 : 3, PTERMS = sizeof(T) == 2 ? 2 : 3;
   constexpr int NT = 4 * NJ;                        // tiles of 16 dimensions
-  // Two tiles of bf16 queries lie in LDS, where the waves join their results later (it has room for them: 17 rows or
-  // more of d floats from every wave): in registers 26 others were spilled (8 query tokens, as above: 416 us).
-  constexpr bool Q_LDS = QT == 2 && sizeof(T) == 2;
+  // bf16 queries lie in LDS where they would make registers spill: two tiles of them (26 spilled; 8 query tokens, as above:
+  // 416 us), where the waves join their results later (17 rows or more of d floats from every wave are room enough),
+  // and those of d = 144 to 176 (12 spilled), in LDS of their own.
+  constexpr bool Q_LDS = sizeof(T) == 2 && (QT == 2 || (NJ == 3 && !EXACT));
   extern __shared__ __align__(16) float lds[];      // [waves][nq][d], nq = query rows of this workgroup; at kept [kept_blocks][nq][64]
   __shared__ float sm[CA_WAVES][16 * QT], sl[CA_WAVES][16 * QT], lse2[16 * QT];
   const CacheView& c = a.c;
@@ -257,7 +258,8 @@ __global__ __launch_bounds__(CA_THREADS, attend_waves(NJ, QT, sizeof(T))) void a
 
   // ---- queries: lane col holds row col, dimensions 64 j + 16 g + 8 half (q_lds: its own 16 bytes of every piece) ----
   bf16x8_t q[QT][NJ][2][TERMS];
-  u32x4_t* const q_lds = reinterpret_cast<u32x4_t*>(lds) + lane;
+  __shared__ u32x4_t q_own[Q_LDS && QT == 1 ? 2 * NJ * 64 : 1];
+  u32x4_t* const q_lds = (QT == 1 ? q_own : reinterpret_cast<u32x4_t*>(lds)) + lane;
   int limit[QT];                                    // tokens that the lane's query sees (of them, those below len are read)
 #pragma unroll
   for (int t = 0; t < QT; ++t) {

@@ -143,3 +143,27 @@ def test_ordinary_rows(fmt, dtype, lens, hkv, group, window, d):
         mine, mine_lse, _ = call_attend(c, q, lens, dtype, causal=int(window > 1), weights=weights)
         print("largest share of the bounds", (np.abs(mine - out) / tol).max(), flush=True)
         assert (np.abs(mine - out) <= tol).all() and (np.abs(mine_lse - lse) <= tol_lse).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,d,group,window", [(orc.E4M3, 144, 16, 1), (orc.INT8, 160, 5, 3), (orc.E4M3, 176, 4, 4), (orc.E4M3, 128, 8, 4),
+                                                (orc.INT8, 80, 17, 1)])
+def test_weights_with_all_of_lds(fmt, d, group, window):
+    """Whole rows whose logits fill what LDS the waves' outputs and the queries leave, and go on in the workspace."""
+    rng = np.random.default_rng([76, d])
+    lens = [int(x) for x in rng.integers(0, 200, 32)]
+    lens[7], lens[31] = 2100, 2000
+    c = random_cache(rng, fmt, lens, 8, d, 1)
+    q = rounded(rng.standard_normal((32, 8 * group, window, d)), "bf16")
+    out, lse, got, mean_abs, largest = orc.attend(c, 0, q, lens, d ** -0.5, causal=window > 1)
+    tol, tol_lse = attend_bounds(c, lens, mean_abs, largest, out, lse, "bf16")
+    mine, mine_lse, gathered = call_attend(c, q, lens, "bf16", causal=int(window > 1))
+    fine = np.isfinite(lse)
+    assert (np.isneginf(mine_lse) == ~fine).all() and (np.abs(mine - out) <= tol).all()
+    assert (np.abs(mine_lse[fine] - lse[fine]) <= tol_lse[fine]).all()
+    for (row, hh), x in got.items():
+        at = c.table[row, :-(-len(x) // 64)]
+        want = c.weight[at, hh].astype(np.float64).ravel()[:len(x)] + x
+        error = np.abs(gathered[at, hh].ravel()[:len(x)] - want)
+        # every probability is as far off as its logit and the log-sum-exp, and one sum of up to 32 of them
+        assert (error <= x * (2 * tol_lse[fine].max() + 40 * 2.0 ** -23) + want * 2.0 ** -23 + 1e-37).all()
