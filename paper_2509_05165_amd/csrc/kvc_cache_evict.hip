@@ -220,7 +220,8 @@ __device__ __forceinline__ float lane_float(float x, int lane) {
 
 // blockDim: 64 * waves, waves = d / 64 rounded up.  magic: 65536 / (d / 16) rounded up.  VALUES: V, else K.
 // Bound by HBM: K 5.0 TB/s, V 4.8 TB/s of the bytes that it moves, which are those of every source block that
-// a kept token lies in.
+// a kept token lies in, and of no other: 64 tokens at the two ends of 131072 (32 rows of 8 heads) take 398 us, most of it the
+// selection, and 2150 if every block between them is walked over.
 template <int FMT, bool VALUES>
 __global__ __launch_bounds__(EM_THREADS) void evict_move(EvictArgs a, int blocks, int64_t units, uint32_t magic) {
   extern __shared__ __align__(16) uint8_t smem[];   // EM_WAVE_LDS per wave
@@ -313,25 +314,24 @@ __global__ __launch_bounds__(EM_THREADS) void evict_move(EvictArgs a, int blocks
             next[n] = *reinterpret_cast<const u32x4_t*>(
                 c.v + (((size_t)from_id * c.hb + hh) * d + min(64 * wave + 16 * n + r4, d - 1)) * CB_TOKENS + 16 * piece);
       };
-      const int last = __builtin_amdgcn_readlane(page, here - 1);
-      int p0 = __builtin_amdgcn_readfirstlane(page);
-      load(p0);
-      int done = 0;                                 // tokens of earlier source blocks
+      load(__builtin_amdgcn_readfirstlane(page));
+      int done = 0;                                 // tokens of earlier source blocks; token `done` lies in the next one
       uint32_t acc = 0;                             // bytes that wait for a full word
-      for (; p0 <= last; p0 += 4) {                 // uniform; four source blocks at a time
+      while (done < here) {                         // uniform; the next four source blocks that hold a kept token
         // which slots of a block stay: every kept token raises the flag of the lane of its slot
         uint64_t mine = 0;
         int before = done;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const bool from_here = page == p0 + g;
+          const int now = done < here ? __builtin_amdgcn_readlane(page, done) : -1;
+          const bool from_here = page == now;
           const int flag = __builtin_amdgcn_ds_permute((from_here ? slot : 0) * 4, from_here ? 1 : 0);
           // lanes without a token of this block push 0 to lane 0, which may win over a flag there
           const uint64_t stay = (__ballot(flag) & ~1ull) | (__ballot(from_here && slot == 0) ? 1ull : 0ull);
           if (lane >> 4 == g) { mine = stay; before = done; }
           done += __popcll(stay);
         }
-        // lane 16 g + i: word i of block p0 + g.  Its n kept bytes follow f that wait.
+        // lane 16 g + i: word i of block g of the four.  Its n kept bytes follow f that wait.
         const int word = lane & 15;
         const uint32_t m4 = (uint32_t)(mine >> (4 * word)) & 15u;
         uint32_t order = 0, n8 = 0;                 // the kept bytes' numbers, 8 n
@@ -347,11 +347,13 @@ __global__ __launch_bounds__(EM_THREADS) void evict_move(EvictArgs a, int blocks
         const uint32_t rest = f8 + n8 < 32 ? fill : f8 ? order >> (32 - f8) : 0u;
         const int at_word = place >> 2;
 #pragma unroll 1
-        for (int g = 0; g < 4 && p0 + g <= last; ++g) {
+        for (int g = 0; g < 4; ++g) {
+          if (__builtin_amdgcn_readlane(before, 16 * g) >= here) break;   // no such block
+          const int next_token = g < 3 ? __builtin_amdgcn_readlane(before, 16 * g + 16) : done;
 #pragma unroll
           for (int n = 0; n < 4; ++n)               // pieces change places so that the reads below meet no bank twice
             *reinterpret_cast<u32x4_t*>(stage + (16 * n + r4) * 64 + ((piece ^ (r4 >> 2 & 3)) << 4)) = next[n];
-          if (p0 + g < last) load(p0 + g + 1);
+          if (next_token < here) load(__builtin_amdgcn_readlane(page, next_token));
           u32x4_t x[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) x[q] = *reinterpret_cast<const u32x4_t*>(stage + lane * 64 + ((q ^ (lane >> 2 & 3)) << 4));
