@@ -291,7 +291,8 @@ kvc_status kvc_compress(const kvc_params* params, const kvc_inputs* in,
  *
  * A code stands for code * scale.  Scales are powers of two: the least 2^e, e >= -100, for which the
  * block's largest magnitude is at most top * 2^e (top = 448 for KVC_E4M3, 127 for KVC_INT8); codes are
- * value / scale rounded to nearest, halves to even.  Non-finite values are undefined.
+ * value / scale rounded to nearest, halves to even.  Non-finite values are undefined, but a weight may be
+ * +infinity (S of the pass's forced tokens).
  *
  * Nothing is read or written outside the pools whatever lengths and table hold: a length is taken
  * between 0 and table_width*64, and a table entry outside [0, blocks) is not followed (its tokens are
@@ -323,7 +324,7 @@ typedef struct kvc_cache {
 
 /* Stage 5 into the cache: rows idx[l,h,0..N_{b,l}) of K and V, in that order or (params->order =
  * KVC_ORDER_POSITION) in ascending position, become the tokens of their row.  Arguments as those of
- * kvc_gather, in whose place it stands; idx may be NULL: the first N_{b,l} tokens as they lie.  The
+ * kvc_gather, in whose place it stands; v must be given; idx may be NULL: the first N_{b,l} tokens as they lie.  The
  * rest of a row's last block is cleared.  Where the cache has weights, a token starts with
  * scores[l,h,position] (scores: device float [Lyr,Hkv,T], for instance S), or 0 if scores is NULL. */
 kvc_status kvc_cache_fill(const kvc_params* params, const void* const* k, const void* const* v,
@@ -371,7 +372,8 @@ kvc_status kvc_cache_attend_workspace(const kvc_params* params, int64_t max_leng
  * keep their order and weights.  keep: device int32 [rows].  The kept tokens are written to the blocks
  * of table_out (device int32 [rows, table_width], same pools), none of which may belong to a row of
  * the table; the rest of a last block is cleared, lengths_out[row] is set and must not be lengths.
- * A value keeps its code times scale exactly unless its new block has a larger scale. */
+ * A value keeps its code times scale exactly unless its new block has a larger scale.  Tokens of absent blocks
+ * go first; one that stays all the same is a token of zeros and weight 0 from then on. */
 kvc_status kvc_cache_evict(const kvc_params* params, const int32_t* lengths, const int32_t* keep,
                            int64_t max_keep, const kvc_cache* cache, const int32_t* table_out,
                            int32_t* lengths_out, void* workspace, size_t workspace_bytes,

@@ -16,7 +16,8 @@
 // of the 16 consecutive tokens of its group, in the order in which the second product wants them as
 // its operand, and with one query: the softmax needs two cross-lane steps per block and the probabilities
 // none.  The other operand, V transposed, is 16 consecutive bytes of a dimension's row of the block.
-// Nothing goes through LDS before the four waves of a workgroup join their results.
+// Codes and probabilities never go through LDS: the queries of some forms do (Q_LDS), logits that a workgroup keeps for
+// the weights of its row (kept), and what the four waves join.
 //
 // Work is split over the tokens: a workgroup takes `chunk` blocks of one head (its waves every fourth
 // one); attend_join adds the splits of a row and, where weights are gathered, turns the stored
