@@ -600,7 +600,7 @@ __global__ __launch_bounds__(CA_THREADS) void attend_join(AttendArgs a, int64_t 
 // of up to 256 blocks stay whole (whole / split, us): 64 x 4000 tokens of 32/8 heads 91 / 115, of 64/8 heads (126 KB of
 // logits, one workgroup to a compute unit) 116 / 131; 32 x 1500 26 / 33; 64 x 8000 218 / 231; 64 x 8192..16384 323 / 360
 // (16 KB of LDS 364, 64 KB 342); 256 x 2800..14000 900 / 1135; 32 x 16384 206 / 229; but short rows only if all
-// their logits fit: 256 x 100..1000 with 32 query rows to a head 175 / 141; and with 128 heads it does not pay: 16 x 4000
+// their logits fit: 256 x 100..1000 with 32 query rows to a head 203 / 158; and with 128 heads it does not pay: 16 x 4000
 // 46 / 36.
 // The workspace is that of the most splits that any shorter max_length asks for, with its logits.
 constexpr int64_t CA_LDS = 152 << 10;               // of 160 KB
